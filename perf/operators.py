@@ -316,12 +316,12 @@ def _own(s):
         return s["d_logits"]
     if "desc" not in s:
         s["desc"] = rv.HeadDesc(case["c"], case["classes"])
-        saved, fwd, bwd = rv.revnet_head_workspace_bytes(s["desc"], case["n"], case["h"], case["w"])
+        saved, nbytes = rv.revnet_head_workspace_bytes(s["desc"], case["n"], case["h"], case["w"])
         s["saved"] = torch.empty(saved, dtype=torch.uint8, device=DEVICE)
-        _workspace(s, max(fwd, bwd))
+        _workspace(s, nbytes)
         s["params"] = rv.pack_head(dict(gamma=s["gamma"], beta=s["beta"], w=s["weight"], b=s["bias"]))
         s["grads"] = rv.pack_head(dict(gamma=s["d_gamma"], beta=s["d_beta"], w=s["d_weight"], b=s["d_bias"]))
-    rv.revnet_head_fwd(s["desc"], s["x"], s["params"], s["logits"], s["saved"], s["ws"], stream)
+    rv.revnet_head_fwd(s["desc"], s["x"], s["params"], s["logits"], s["saved"], stream)
     rv.revnet_head_bwd(s["desc"], s["x"], s["saved"], s["dlogits"], s["params"], s["dx"], s["grads"], 0, s["ws"], stream)
     return [s["logits"], s["dx"], s["d_gamma"], s["d_beta"], s["d_weight"], s["d_bias"]]
 
