@@ -453,6 +453,198 @@ int revnet_stack_bwd_fixed(const rvn_block_desc *desc, int32_t depth, int32_t fr
                            const rvn_block_grads *grads, int accumulate_wgrads,
                            void *ws, size_t ws_bytes, void *hip_stream);
 
+/* ------------------------------------------------------------------------
+ * Activation checkpoints in 8 bits.
+ *
+ * A checkpoint holds a tensor [n, c, h, w] as signed 8-bit codes q and one fp32
+ * scale s for each group of RVN_CKPT_GROUP consecutive pixels of a plane (the
+ * last group of a plane may be shorter); a code stands for the fp32 product
+ * q * s.  With A the largest magnitude of the group (at least 126 * 2^-126):
+ *     s = A / 126,   q = rint(x * (126 / A)),   |q| <= 126,
+ * every operation rounded to fp32 once, to nearest even: a value is off by at
+ * most half a scale, A / 252.  A group that holds an infinity or a NaN gets
+ * the scale NaN and codes 0: all of it reads back as NaN.
+ *
+ * Given the batch statistics of a BN + ReLU layer that reads the tensor
+ * (`stats`: four arrays of c floats, one after the other: mean, rstd =
+ * 1 / sqrt(var + eps), scale = gamma * rstd, shift = beta - mean * scale), the
+ * ReLU's decisions are kept as well: a(x) = max(x * scale + shift, 0) is
+ * positive for the value that was saved exactly where it is positive for the
+ * value read back (x * scale + shift is one fused multiply-add in both).  A
+ * code on the wrong side of the border moves one step (then |q| <= 127, and
+ * the value is off by at most a scale).
+ *
+ * Memory: codes [n][c][h*w] (int8, dense), zero to 255 unused bytes up to the
+ * next multiple of 256, scales [n][c][ceil(h*w / RVN_CKPT_GROUP)] (fp32, dense).
+ * ckpt: device, 256-byte aligned, at least revnet_ckpt_bytes of it, which must
+ * not overlap a tensor of the same call.  Errors as for the other entry points.
+ * ---------------------------------------------------------------------- */
+#define RVN_CKPT_GROUP 128
+int revnet_ckpt_bytes(int64_t n, int64_t c, int64_t h, int64_t w, size_t *bytes);
+
+/* Saves x.  stats: NULL, or the statistics of the layer that reads x, as above. */
+int revnet_ckpt_save(const rvn_tensor *x, const float *stats, void *ckpt, size_t ckpt_bytes, void *hip_stream);
+
+/* x (written, any supported strides) = the values that the codes stand for; x's shape is the saved tensor's. */
+int revnet_ckpt_load(const void *ckpt, size_t ckpt_bytes, const rvn_tensor *x, void *hip_stream);
+
+/*
+ * Backward pass of a(x) = ReLU(BN(x)) from a checkpoint of x, with nothing
+ * decoded to memory: from da, the derivative with respect to a,
+ *     dz = da where x * scale + shift > 0, else 0;   xh = (x - mean) * rstd
+ *     d_beta (+)= sum dz,   d_gamma (+)= sum dz * xh     (sums over n, h, w)
+ *     dx = [skip +] scale * (dz - mean(dz) - xh * mean(dz * xh))
+ * with `stats` as for revnet_ckpt_save.  da, skip (NULL: none): read.  dx:
+ * written; it may be the same tensor as da or skip (same ptr and strides), any
+ * other overlap is RVN_ERR_ALIAS.  d_gamma, d_beta [c]: overwritten, or added
+ * to when accumulate != 0.  ws: 256-byte aligned, of the size that
+ * revnet_ckpt_bn_relu_workspace_bytes reports.
+ */
+int revnet_ckpt_bn_relu_workspace_bytes(int64_t n, int64_t c, int64_t h, int64_t w, size_t *bytes);
+int revnet_ckpt_bn_relu_bwd(const void *ckpt, size_t ckpt_bytes, const float *stats,
+                            const rvn_tensor *da, const rvn_tensor *skip, const rvn_tensor *dx,
+                            float *d_gamma, float *d_beta, int accumulate,
+                            void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Stacks and bodies that store instead of recompute: the other end of the
+ * trade of Section 3.2, for callers with memory to spare.  The forward pass
+ * gives the bits of revnet_stack_fwd / revnet_body_fwd and also leaves, in
+ * `store`, a checkpoint and the batch statistics of the input of every layer;
+ * the backward pass reads those and evaluates no function again (2 of the
+ * reversible backward pass's 3 units of work).  It needs neither the top
+ * activations of a stack nor its input, and reconstructs neither.  ReLU
+ * decisions and batch statistics are the forward pass's own; what the 8 bits
+ * round is the activation that a filter gradient multiplies and the xh of the
+ * BN backward pass.  `store` is a buffer of the caller's, device, 256-byte
+ * aligned, of store_bytes, which grow with the depth (a byte for every element
+ * of every layer's input); the library alone knows its layout.  One call of the
+ * backward pass reads it and leaves it as it was.
+ */
+int revnet_stack_stored_bytes(const rvn_block_desc *desc, int32_t depth, int64_t n, int64_t h, int64_t w,
+                              size_t *store_bytes, size_t *fwd_ws_bytes, size_t *bwd_ws_bytes);
+int revnet_stack_fwd_stored(const rvn_block_desc *desc, int32_t depth,
+                            const rvn_tensor *x1, const rvn_tensor *x2,
+                            const rvn_block_params *params,
+                            const rvn_tensor *y1, const rvn_tensor *y2,
+                            void *store, size_t store_bytes,
+                            void *ws, size_t ws_bytes, void *hip_stream);
+/* dx_i may be the same tensor as dy_i; any other overlap is RVN_ERR_ALIAS. */
+int revnet_stack_bwd_stored(const rvn_block_desc *desc, int32_t depth,
+                            const rvn_tensor *dy1, const rvn_tensor *dy2,
+                            const rvn_block_params *params,
+                            const rvn_tensor *dx1, const rvn_tensor *dx2,
+                            const rvn_block_grads *grads, int accumulate_wgrads,
+                            const void *store, size_t store_bytes,
+                            void *ws, size_t ws_bytes, void *hip_stream);
+
+/* The same for a body (see revnet_body_fwd, revnet_body_bwd).  The inputs of the
+ * subsampling blocks stay stored as they are there, in fp32: tops must be kept
+ * for the backward pass, which does not change them. */
+int revnet_body_stored_bytes(const rvn_body_desc *desc, int64_t n, int64_t h, int64_t w,
+                             size_t *store_bytes, size_t *fwd_ws_bytes, size_t *bwd_ws_bytes);
+int revnet_body_fwd_stored(const rvn_body_desc *desc, const rvn_tensor *x,
+                           const rvn_block_params *const *stage_params, const rvn_down_params *down_params,
+                           const rvn_tensor *tops, void *store, size_t store_bytes,
+                           void *ws, size_t ws_bytes, void *hip_stream);
+int revnet_body_bwd_stored(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_tensor *dtops,
+                           const rvn_block_params *const *stage_params, const rvn_down_params *down_params,
+                           const rvn_block_grads *const *stage_grads, const rvn_down_grads *down_grads,
+                           int accumulate_wgrads, const void *store, size_t store_bytes,
+                           void *ws, size_t ws_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
+ * Classification: head, log probabilities, and their gradients.
+ * ---------------------------------------------------------------------- */
+
+/* Device matrix [rows][cols], ld >= cols elements from row to row, columns
+ * contiguous; ptr aligned to its elements. */
+typedef struct {
+    void *ptr;
+    rvn_dtype dtype;
+    int64_t rows, cols, ld;
+} rvn_matrix;
+
+/*
+ * Head: the network's last layers, after the body (the paper follows the
+ * residual networks it cites): logits = fc(mean over pixels of ReLU(BN(x))).
+ * x [n, c, h, w] is the last stage's top (n*h*w up to 2^31-1, n up to 65535);
+ * logits fp32 [n][classes].  `saved` is a buffer of the caller's (256-byte
+ * aligned, saved_bytes) that carries the batch statistics and the pooled values
+ * from revnet_head_fwd to revnet_head_bwd.  All arithmetic is fp32.
+ */
+typedef struct {
+    int32_t c, classes;
+    float bn_eps;
+} rvn_head_desc;
+typedef struct {
+    const float *bn_gamma, *bn_beta; /* [c] */
+    const float *fc_w;               /* [classes][c] */
+    const float *fc_b;               /* [classes] */
+} rvn_head_params;
+typedef struct {
+    float *d_bn_gamma, *d_bn_beta, *d_fc_w, *d_fc_b;
+} rvn_head_grads;
+
+/* Either output pointer may be NULL. */
+int revnet_head_workspace_bytes(const rvn_head_desc *desc, int64_t n, int64_t h, int64_t w,
+                                size_t *saved_bytes, size_t *bwd_bytes);
+int revnet_head_fwd(const rvn_head_desc *desc, const rvn_tensor *x, const rvn_head_params *params,
+                    const rvn_matrix *logits, void *saved, size_t saved_bytes, void *hip_stream);
+/*
+ * From x as it was in the forward pass, `saved` and d_logits [n][classes]: dx
+ * (written; no overlap with x) and the parameter gradients (overwritten, or
+ * added to when accumulate_wgrads != 0).  ws: bwd_bytes, 256-byte aligned.
+ */
+int revnet_head_bwd(const rvn_head_desc *desc, const rvn_tensor *x, const void *saved, size_t saved_bytes,
+                    const rvn_matrix *d_logits, const rvn_head_params *params, const rvn_tensor *dx,
+                    const rvn_head_grads *grads, int accumulate_wgrads,
+                    void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Log probabilities of given labels (class or token numbers) under the softmax
+ * of each row of `logits` (fp32 or bf16, [rows][classes], classes < 2^31), with
+ * the entropy of the row's distribution, the logarithm of its normaliser and
+ * its most likely classes, in one pass over the logits:
+ *     lse = log sum_j exp(x_j),  logprob = x_label - lse,
+ *     entropy = -sum_j p_j log p_j,  p_j = exp(x_j - lse)
+ * labels [rows]: RVN_NO_LABEL marks a row without one (logprob 0); any other
+ * number outside [0, classes) gives NaN.  top_ids, top_logprob [rows][top_k]:
+ * the top_k largest logits' classes in falling order, the lower class first
+ * among equals, and their log probabilities; 0 <= top_k <= min(classes,
+ * RVN_MAX_TOP_K).  Every output is fp32 (ids int64) and may be NULL (labels and
+ * logprob both or neither; with top_k > 0 top_ids is needed) but not all are.
+ * A logit of -infinity is a class that cannot occur; a row with no other has
+ * lse and log probabilities of -infinity and entropy 0.  A row that holds a NaN
+ * or +infinity gets NaN for all but its ids (NaN counts as the largest).
+ * ws: revnet_logprob_workspace_bytes (which may be 0: ws is then not looked
+ * at), 256-byte aligned.
+ */
+#define RVN_NO_LABEL (-1)
+#define RVN_MAX_TOP_K 32
+int revnet_logprob_workspace_bytes(int64_t rows, int64_t classes, int32_t top_k, size_t *bytes);
+int revnet_logprob_fwd(const rvn_matrix *logits, const int64_t *labels, int32_t top_k,
+                       float *logprob, float *entropy, float *lse, int64_t *top_ids, float *top_logprob,
+                       void *ws, size_t ws_bytes, void *hip_stream);
+
+/*
+ * Gradient of scale * sum_rows (d_logprob * logprob + d_entropy * entropy) with
+ * respect to the logits, from the forward pass's lse (and entropy, needed with
+ * d_entropy):
+ *     d_logits_j = scale * (d_logprob * (delta_j,label - p_j)
+ *                           - d_entropy * p_j * (log p_j + entropy))
+ * d_logprob [rows]: NULL = 1 for every row (scale = -1 / rows then gives the
+ * gradient of the mean negative log likelihood); d_entropy [rows]: NULL = 0.
+ * labels as above; NULL: the logprob term is absent.  Rows without a label take
+ * part in the entropy term only; a row whose label is out of range gets NaN.
+ * d_logits has the logits' shape and type and may be the same matrix (same ptr
+ * and ld); any other overlap is RVN_ERR_ALIAS.  A row of -infinity alone gets
+ * zeros.
+ */
+int revnet_logprob_bwd(const rvn_matrix *logits, const int64_t *labels, const float *lse, const float *entropy,
+                       const float *d_logprob, const float *d_entropy, float scale,
+                       const rvn_matrix *d_logits, void *hip_stream);
+
 /*
  * What revnet_stack_fwd (fwd) and revnet_stack_bwd (bwd) would enqueue for
  * this descriptor, depth and half-tensor shape, without touching the device.

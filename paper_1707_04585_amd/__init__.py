@@ -13,4 +13,9 @@ from .binding import (  # noqa: F401
     revnet_stack_fwd_fixed, revnet_stem_bwd, revnet_stem_fwd, revnet_stem_workspace_bytes, rvn_stem_desc,
     revnet_body_bwd_fixed, revnet_body_fixed_workspace_bytes, revnet_body_fwd_fixed,
     revnet_stack_fwd_static, STATIC_WS_BYTES,
+    CKPT_GROUP, revnet_ckpt_bn_relu_bwd, revnet_ckpt_bn_relu_workspace_bytes, revnet_ckpt_bytes, revnet_ckpt_load, revnet_ckpt_save,
+    revnet_body_bwd_stored, revnet_body_fwd_stored, revnet_body_stored_bytes,
+    revnet_stack_bwd_stored, revnet_stack_fwd_stored, revnet_stack_stored_bytes,
+    HeadDesc, pack_head, revnet_head_bwd, revnet_head_fwd, revnet_head_workspace_bytes, rvn_head_desc,
+    MAX_TOP_K, NO_LABEL, revnet_logprob_bwd, revnet_logprob_fwd, revnet_logprob_workspace_bytes, rvn_matrix,
 )

@@ -29,8 +29,16 @@ EXPORTS = [
     "revnet_stem_workspace_bytes", "revnet_stem_fwd", "revnet_stem_bwd",
     "revnet_body_fixed_workspace_bytes", "revnet_body_fwd_fixed", "revnet_body_bwd_fixed",
     "revnet_stack_fwd_static",
+    "revnet_ckpt_bytes", "revnet_ckpt_save", "revnet_ckpt_load", "revnet_ckpt_bn_relu_workspace_bytes", "revnet_ckpt_bn_relu_bwd",
+    "revnet_stack_stored_bytes", "revnet_stack_fwd_stored", "revnet_stack_bwd_stored",
+    "revnet_body_stored_bytes", "revnet_body_fwd_stored", "revnet_body_bwd_stored",
+    "revnet_head_workspace_bytes", "revnet_head_fwd", "revnet_head_bwd",
+    "revnet_logprob_workspace_bytes", "revnet_logprob_fwd", "revnet_logprob_bwd",
 ]
 STATIC_WS_BYTES = 32 << 20   # RVN_STATIC_WS_BYTES
+CKPT_GROUP = 128             # RVN_CKPT_GROUP
+NO_LABEL = -1                # RVN_NO_LABEL
+MAX_TOP_K = 32               # RVN_MAX_TOP_K
 
 MAX_STAGES = 8
 
@@ -74,6 +82,18 @@ class rvn_body_desc(C.Structure):
 
 class rvn_stem_desc(C.Structure):
     _fields_ = [("c_in", C.c_int32), ("c_out", C.c_int32), ("ks", C.c_int32), ("stride", C.c_int32), ("pool", C.c_int32)]
+
+
+class rvn_matrix(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("dtype", C.c_int), ("rows", C.c_int64), ("cols", C.c_int64), ("ld", C.c_int64)]
+
+
+class rvn_head_desc(C.Structure):
+    _fields_ = [("c", C.c_int32), ("classes", C.c_int32), ("bn_eps", C.c_float)]
+
+
+class rvn_head_ptrs(C.Structure):  # rvn_head_params / rvn_head_grads
+    _fields_ = [(k, C.c_void_p) for k in ("bn_gamma", "bn_beta", "fc_w", "fc_b")]
 
 
 class rvn_cost(C.Structure):
@@ -153,8 +173,18 @@ class BodyDesc:
         return out
 
 
+class HeadDesc:
+    """Classification head on c channels."""
+
+    def __init__(self, channels, classes, bn_eps=1e-5):
+        self.channels, self.classes, self.bn_eps = int(channels), int(classes), float(bn_eps)
+
+    def c(self):
+        return rvn_head_desc(self.channels, self.classes, self.bn_eps)
+
+
 def _desc(d):
-    return d.c() if isinstance(d, (BlockDesc, DownDesc, BodyDesc)) else d
+    return d.c() if isinstance(d, (BlockDesc, DownDesc, BodyDesc, HeadDesc)) else d
 
 
 def _tensor(t):
@@ -235,6 +265,34 @@ def _tensor_array(ts):
     for i, t in enumerate(ts):
         arr[i] = _tensor(t)
     return arr
+
+
+def _is(t, dtype):
+    return str(t.dtype) == "torch." + dtype
+
+
+def _matrix(t, name):
+    if t is None or isinstance(t, rvn_matrix):
+        return t
+    rows, cols = t.shape
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
+        raise ValueError(f"the columns of {name} must be contiguous")
+    dtype = F32 if _is(t, "float32") else BF16 if _is(t, "bfloat16") else -1
+    return rvn_matrix(t.data_ptr(), dtype, rows, cols, ld if rows > 1 else max(ld, cols))
+
+
+def _vector(t, name, count, dtype="float32"):
+    """Device pointer of a dense array of `count` elements (an integer is passed through as a pointer)."""
+    if t is None or isinstance(t, int):
+        return t
+    if not _is(t, dtype) or t.numel() != count or not t.is_contiguous():
+        raise ValueError(f"{name} must be {count} contiguous elements of {dtype}")
+    return t.data_ptr()
+
+
+def _by_ref(t):
+    return None if t is None else C.byref(t)
 
 
 def _stream(stream):
@@ -491,6 +549,167 @@ def revnet_stem_bwd(desc, img, conv_out, dy, d_w, accumulate_wgrads, ws, stream=
     _check(load_library().revnet_stem_bwd(C.byref(desc), C.byref(ti), _opt_tensor(conv_out), C.byref(td),
                                           C.c_void_p(_ptr(d_w)), C.c_int(int(accumulate_wgrads)), C.c_void_p(wp),
                                           C.c_size_t(wb), C.c_void_p(_stream(stream))))
+
+
+def revnet_ckpt_bytes(n, c, h, w):
+    out = C.c_size_t(0)
+    _check(load_library().revnet_ckpt_bytes(C.c_int64(n), C.c_int64(c), C.c_int64(h), C.c_int64(w), C.byref(out)))
+    return int(out.value)
+
+
+def revnet_ckpt_save(x, stats, ckpt, stream=None):
+    """stats: None, or a [4, c] tensor (mean, rstd, scale, shift)."""
+    tx = _tensor(x)
+    kp, kb = _ws(ckpt)
+    _check(load_library().revnet_ckpt_save(C.byref(tx), C.c_void_p(_vector(stats, "stats", 4 * tx.c)), C.c_void_p(kp), C.c_size_t(kb),
+                                           C.c_void_p(_stream(stream))))
+
+
+def revnet_ckpt_load(ckpt, x, stream=None):
+    tx = _tensor(x)
+    kp, kb = _ws(ckpt)
+    _check(load_library().revnet_ckpt_load(C.c_void_p(kp), C.c_size_t(kb), C.byref(tx), C.c_void_p(_stream(stream))))
+
+
+def revnet_ckpt_bn_relu_workspace_bytes(n, c, h, w):
+    out = C.c_size_t(0)
+    _check(load_library().revnet_ckpt_bn_relu_workspace_bytes(C.c_int64(n), C.c_int64(c), C.c_int64(h), C.c_int64(w), C.byref(out)))
+    return int(out.value)
+
+
+def revnet_ckpt_bn_relu_bwd(ckpt, stats, da, skip, dx, d_gamma, d_beta, accumulate, ws, stream=None):
+    ta, tx = _tensor(da), _tensor(dx)
+    ts = None if skip is None else _tensor(skip)
+    kp, kb = _ws(ckpt)
+    wp, wb = _ws(ws)
+    _check(load_library().revnet_ckpt_bn_relu_bwd(
+        C.c_void_p(kp), C.c_size_t(kb), C.c_void_p(_vector(stats, "stats", 4 * ta.c)), C.byref(ta), _by_ref(ts), C.byref(tx),
+        C.c_void_p(_vector(d_gamma, "d_gamma", ta.c)), C.c_void_p(_vector(d_beta, "d_beta", ta.c)), C.c_int(int(accumulate)),
+        C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+
+
+def revnet_stack_stored_bytes(desc, depth, n, h, w):
+    """-> (store, forward workspace, backward workspace)"""
+    out = [C.c_size_t(0) for _ in range(3)]
+    d = _desc(desc)
+    _check(load_library().revnet_stack_stored_bytes(C.byref(d), C.c_int32(depth), C.c_int64(n), C.c_int64(h), C.c_int64(w),
+                                                    *[C.byref(v) for v in out]))
+    return tuple(int(v.value) for v in out)
+
+
+def revnet_stack_fwd_stored(desc, depth, x1, x2, params, y1, y2, store, ws, stream=None):
+    d = _desc(desc)
+    p = pack_params(params)
+    sp, sb = _ws(store)
+    wp, wb = _ws(ws)
+    t = [_tensor(v) for v in (x1, x2, y1, y2)]
+    _check(load_library().revnet_stack_fwd_stored(C.byref(d), C.c_int32(depth), C.byref(t[0]), C.byref(t[1]), p, C.byref(t[2]),
+                                                  C.byref(t[3]), C.c_void_p(sp), C.c_size_t(sb), C.c_void_p(wp), C.c_size_t(wb),
+                                                  C.c_void_p(_stream(stream))))
+
+
+def revnet_stack_bwd_stored(desc, depth, dy1, dy2, params, dx1, dx2, grads, accumulate_wgrads, store, ws, stream=None):
+    d = _desc(desc)
+    p, g = pack_params(params), pack_grads(grads)
+    sp, sb = _ws(store)
+    wp, wb = _ws(ws)
+    t = [_tensor(v) for v in (dy1, dy2, dx1, dx2)]
+    _check(load_library().revnet_stack_bwd_stored(C.byref(d), C.c_int32(depth), C.byref(t[0]), C.byref(t[1]), p, C.byref(t[2]),
+                                                  C.byref(t[3]), g, C.c_int(int(accumulate_wgrads)), C.c_void_p(sp), C.c_size_t(sb),
+                                                  C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+
+
+def revnet_body_stored_bytes(desc, n, h, w):
+    """-> (store, forward workspace, backward workspace)"""
+    out = [C.c_size_t(0) for _ in range(3)]
+    d = _desc(desc)
+    _check(load_library().revnet_body_stored_bytes(C.byref(d), C.c_int64(n), C.c_int64(h), C.c_int64(w), *[C.byref(v) for v in out]))
+    return tuple(int(v.value) for v in out)
+
+
+def revnet_body_fwd_stored(desc, x, stage_params, down_params, tops, store, ws, stream=None):
+    d = _desc(desc)
+    sp, keep = pack_stages(stage_params)
+    dp = pack_down(down_params)
+    kp, kb = _ws(store)
+    wp, wb = _ws(ws)
+    tx, tt = _tensor(x), _tensor_array(tops)
+    _check(load_library().revnet_body_fwd_stored(C.byref(d), C.byref(tx), sp, dp, tt, C.c_void_p(kp), C.c_size_t(kb), C.c_void_p(wp),
+                                                 C.c_size_t(wb), C.c_void_p(_stream(stream))))
+    del keep
+
+
+def revnet_body_bwd_stored(desc, tops, dtops, stage_params, down_params, stage_grads, down_grads, accumulate_wgrads, store, ws,
+                           stream=None):
+    d = _desc(desc)
+    sp, keep_p = pack_stages(stage_params)
+    sg, keep_g = pack_stages(stage_grads)
+    dp, dg = pack_down(down_params), pack_down(down_grads)
+    kp, kb = _ws(store)
+    wp, wb = _ws(ws)
+    tt, td = _tensor_array(tops), _tensor_array(dtops)
+    _check(load_library().revnet_body_bwd_stored(C.byref(d), tt, td, sp, dp, sg, dg, C.c_int(int(accumulate_wgrads)), C.c_void_p(kp),
+                                                 C.c_size_t(kb), C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+    del keep_p, keep_g
+
+
+def pack_head(P) -> rvn_head_ptrs:
+    """{gamma, beta, w, b} of device tensors -> rvn_head_params / rvn_head_grads."""
+    return P if isinstance(P, rvn_head_ptrs) else rvn_head_ptrs(*[_ptr(P[k]) for k in ("gamma", "beta", "w", "b")])
+
+
+def revnet_head_workspace_bytes(desc, n, h, w):
+    """-> (saved, backward workspace)"""
+    saved, bwd = C.c_size_t(0), C.c_size_t(0)
+    d = _desc(desc)
+    _check(load_library().revnet_head_workspace_bytes(C.byref(d), C.c_int64(n), C.c_int64(h), C.c_int64(w), C.byref(saved), C.byref(bwd)))
+    return int(saved.value), int(bwd.value)
+
+
+def revnet_head_fwd(desc, x, params, logits, saved, stream=None):
+    d, p, tx, tl = _desc(desc), pack_head(params), _tensor(x), _matrix(logits, "logits")
+    sp, sb = _ws(saved)
+    _check(load_library().revnet_head_fwd(C.byref(d), C.byref(tx), C.byref(p), _by_ref(tl), C.c_void_p(sp), C.c_size_t(sb),
+                                          C.c_void_p(_stream(stream))))
+
+
+def revnet_head_bwd(desc, x, saved, d_logits, params, dx, grads, accumulate_wgrads, ws, stream=None):
+    d, p, g = _desc(desc), pack_head(params), pack_head(grads)
+    tx, tl, td = _tensor(x), _matrix(d_logits, "d_logits"), _tensor(dx)
+    sp, sb = _ws(saved)
+    wp, wb = _ws(ws)
+    _check(load_library().revnet_head_bwd(C.byref(d), C.byref(tx), C.c_void_p(sp), C.c_size_t(sb), _by_ref(tl), C.byref(p), C.byref(td),
+                                          C.byref(g), C.c_int(int(accumulate_wgrads)), C.c_void_p(wp), C.c_size_t(wb),
+                                          C.c_void_p(_stream(stream))))
+
+
+def revnet_logprob_workspace_bytes(rows, classes, top_k):
+    out = C.c_size_t(0)
+    _check(load_library().revnet_logprob_workspace_bytes(C.c_int64(rows), C.c_int64(classes), C.c_int32(top_k), C.byref(out)))
+    return int(out.value)
+
+
+def revnet_logprob_fwd(logits, labels, top_k, logprob, entropy, lse, top_ids, top_logprob, ws, stream=None):
+    """With top_k == 0 top_ids and top_logprob are not looked at; any other output may be None (labels with logprob)."""
+    m = _matrix(logits, "logits")
+    rows = m.rows if m is not None else 0
+    if top_k == 0:
+        top_ids = top_logprob = None
+    wp, wb = _ws(ws)
+    _check(load_library().revnet_logprob_fwd(
+        _by_ref(m), C.c_void_p(_vector(labels, "labels", rows, "int64")), C.c_int32(top_k),
+        C.c_void_p(_vector(logprob, "logprob", rows)), C.c_void_p(_vector(entropy, "entropy", rows)),
+        C.c_void_p(_vector(lse, "lse", rows)), C.c_void_p(_vector(top_ids, "top_ids", rows * top_k, "int64")),
+        C.c_void_p(_vector(top_logprob, "top_logprob", rows * top_k)), C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+
+
+def revnet_logprob_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, scale, d_logits, stream=None):
+    m, d = _matrix(logits, "logits"), _matrix(d_logits, "d_logits")
+    rows = m.rows if m is not None else 0
+    _check(load_library().revnet_logprob_bwd(
+        _by_ref(m), C.c_void_p(_vector(labels, "labels", rows, "int64")), C.c_void_p(_vector(lse, "lse", rows)),
+        C.c_void_p(_vector(entropy, "entropy", rows)), C.c_void_p(_vector(d_logprob, "d_logprob", rows)),
+        C.c_void_p(_vector(d_entropy, "d_entropy", rows)), C.c_float(scale), _by_ref(d), C.c_void_p(_stream(stream))))
 
 
 def revnet_profile_begin():

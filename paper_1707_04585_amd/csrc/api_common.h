@@ -36,6 +36,9 @@ inline size_t align_up(size_t v) { return (v + kAlign - 1) / kAlign * kAlign; }
 int check_desc(const rvn_block_desc *d);
 int check_geo(int64_t n, int64_t h, int64_t w);
 int check_ws(const void *ws, size_t have, size_t need);
+// A buffer of the caller's that carries state from one call to another (checkpoint, store, what a head saves).
+int check_store(const char *name, const void *p, size_t have, size_t need);
+bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes);
 int check_params(const rvn_block_desc &d, const rvn_block_params *p, const char *what);
 int check_grads(const rvn_block_desc &d, const rvn_block_grads *p, const char *what);
 // Shape [n, c, h, w], the supported strides (sw = 1, sh = w, sc >= h*w, sn >= (c-1)*sc + h*w), alignment.
@@ -95,14 +98,39 @@ Bufs bind(const Plan &p, void *ws);
 int check_fwd_args(const rvn_block_desc *desc, const rvn_tensor *x1, const rvn_tensor *x2, const rvn_tensor *y1,
                    const rvn_tensor *y2, void *ws, size_t ws_bytes, Plan *plan, Geo *geo, bool fixed);
 
+// What a stack that stores instead of recomputing keeps of one residual function: the statistics arrays and the
+// checkpoint of every layer's input.  Offsets in bytes from the function's place in the store; a block holds two
+// functions (F, then G), a stack its blocks in order.
+struct StorePlan {
+    size_t stats[3], codes[3], scales[3];
+    size_t func;                              // bytes of one function
+    size_t stack(int depth) const { return 2 * func * (size_t)depth; }
+};
+StorePlan make_store_plan(const rvn_block_desc &d, const Geo &g);
+// Checkpoint buffers as a caller sees them: codes, then scales from the next multiple of 256 bytes.
+inline size_t ckpt_codes_bytes(int c, const Geo &g) { return align_up((size_t)g.pixels() * (size_t)c); }
+inline size_t ckpt_bytes(int c, const Geo &g) {
+    return ckpt_codes_bytes(c, g) + (size_t)g.n * (size_t)c * (size_t)ckpt_groups(g.hw()) * 4;
+}
+// The backward workspace of a stack that stores: the plan of revnet_stack_bwd, partial sums of the BN backward passes
+// and, where the plan's room for h is too small, a buffer for one decoded layer input.
+struct StoredWs {
+    size_t sums, xf, total;
+};
+StoredWs stored_bwd_ws(const Plan &p, const Geo &g);
+
 // Section 3.2: blocks params[0 .. depth-1] in order, only the top pair kept; and
 // Algorithm 1 applied from the top block down.  frac_bits > 0: the stream
 // tensors hold fixed-point codes.
 void stack_forward(Ctx &cx, const rvn_block_desc &d, int depth, const Plan &pl, const Bufs &b, Geo g, View x1, View x2,
-                   const rvn_block_params *params, View y1, View y2, int frac_bits = 0);
+                   const rvn_block_params *params, View y1, View y2, int frac_bits = 0, char *store = nullptr);
 void stack_backward(Ctx &cx, const rvn_block_desc &d, int depth, const Plan &pl, const Bufs &b, Geo g, View y1, View y2,
                     View dy1, View dy2, const rvn_block_params *params, View x1, View x2, View dx1, View dx2,
                     const rvn_block_grads *grads, bool accumulate, int frac_bits = 0);
+// Backward pass from what stack_forward left in `store`; ws: the base that `b` was bound to.
+void stack_backward_stored(Ctx &cx, const rvn_block_desc &d, int depth, const Plan &pl, const Bufs &b, Geo g, View dy1, View dy2,
+                           const rvn_block_params *params, View dx1, View dx2, const rvn_block_grads *grads, bool accumulate,
+                           const char *store, void *ws);
 
 }  // namespace api
 }  // namespace rvn

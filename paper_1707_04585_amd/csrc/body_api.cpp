@@ -360,6 +360,23 @@ BodyWs body_ws(const rvn_body_desc &bd, const Geo &g0, bool backward, bool fixed
     return w;
 }
 
+// A body that stores: the stages' stores one after the other, and the backward workspace's largest need.
+size_t body_store_at(const rvn_body_desc &bd, const Geo &g0, int stage) {
+    size_t off = 0;
+    for (int s = 0; s < stage; ++s)
+        off += make_store_plan(bd.stage[s], Geo{g0.n, g0.h >> s, g0.w >> s}).stack(bd.depth[s]);
+    return off;
+}
+
+size_t body_stored_bwd_bytes(const rvn_body_desc &bd, const Geo &g0) {
+    size_t most = body_ws(bd, g0, true, false).total;
+    for (int s = 0; s < bd.stages; ++s) {
+        const Geo g{g0.n, g0.h >> s, g0.w >> s};
+        most = std::max(most, stored_bwd_ws(make_plan(bd.stage[s], g, true), g).total);
+    }
+    return most;
+}
+
 size_t body_ws_bytes(const rvn_body_desc &bd, const Geo &g0, bool backward, bool fixed = false) {
     return body_ws(bd, g0, backward, fixed).total;
 }
@@ -459,7 +476,7 @@ namespace {
 // encoded into the next stage's tensor).
 int body_fwd_impl(const rvn_body_desc *desc, const rvn_tensor *x, const rvn_block_params *const *stage_params,
                   const rvn_down_params *down_params, const rvn_tensor *tops, void *ws, size_t ws_bytes,
-                  void *hip_stream, int frac_bits) {
+                  void *hip_stream, int frac_bits, bool storing = false, void *store = nullptr, size_t store_bytes = 0) {
     if (!x) return fail(RVN_ERR_NULL, "tensor x is NULL");
     if (int rc = check_body_desc(desc, x->n, x->h, x->w)) return rc;
     const rvn_body_desc &bd = *desc;
@@ -483,6 +500,14 @@ int body_fwd_impl(const rvn_body_desc *desc, const rvn_tensor *x, const rvn_bloc
     if (overlaps_range(x, ws, need)) return fail(RVN_ERR_ALIAS, "x overlaps the workspace");
     for (int s = 0; s < bd.stages; ++s)
         if (overlaps_range(&tops[s], ws, need)) return fail(RVN_ERR_ALIAS, "tops[%d] overlaps the workspace", s);
+    if (storing) {
+        const size_t store_need = body_store_at(bd, g0, bd.stages);
+        if (int rc = check_store("store", store, store_bytes, store_need)) return rc;
+        if (ranges_overlap(store, store_need, ws, need)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
+        if (overlaps_range(x, store, store_need)) return fail(RVN_ERR_ALIAS, "x overlaps the store");
+        for (int s = 0; s < bd.stages; ++s)
+            if (overlaps_range(&tops[s], store, store_need)) return fail(RVN_ERR_ALIAS, "tops[%d] overlaps the store", s);
+    }
     Ctx cx;
     cx.stream = static_cast<hipStream_t>(hip_stream);
     for (int s = 0; s < bd.stages; ++s) {
@@ -494,7 +519,8 @@ int body_fwd_impl(const rvn_body_desc *desc, const rvn_tensor *x, const rvn_bloc
             in = &tops[0];
         }
         stack_forward(cx, bd.stage[s], bd.depth[s], pl, bind(pl, ws), g, half_view(in, 0), half_view(in, 1),
-                      stage_params[s], half_view(&tops[s], 0), half_view(&tops[s], 1), frac_bits);
+                      stage_params[s], half_view(&tops[s], 0), half_view(&tops[s], 1), frac_bits,
+                      storing ? static_cast<char *>(store) + body_store_at(bd, g0, s) : nullptr);
         if (s + 1 < bd.stages) {
             const DownPlan dp = make_down_plan(bd.down[s], g, false);
             if (frac_bits) {
@@ -537,7 +563,8 @@ namespace {
 int body_bwd_impl(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_tensor *dtops,
                   const rvn_block_params *const *stage_params, const rvn_down_params *down_params,
                   const rvn_block_grads *const *stage_grads, const rvn_down_grads *down_grads,
-                  int accumulate_wgrads, void *ws, size_t ws_bytes, void *hip_stream, int frac_bits) {
+                  int accumulate_wgrads, void *ws, size_t ws_bytes, void *hip_stream, int frac_bits, bool storing = false,
+                  const void *store = nullptr, size_t store_bytes = 0) {
     if (!tops) return fail(RVN_ERR_NULL, "tops is NULL");
     if (int rc = check_body_desc(desc, tops[0].n, tops[0].h, tops[0].w)) return rc;
     const rvn_body_desc &bd = *desc;
@@ -561,11 +588,19 @@ int body_bwd_impl(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_t
     }
     const Geo g0{(int)n, (int)h, (int)w};
     const BodyWs bw = body_ws(bd, g0, true, frac_bits != 0);
-    const size_t need = bw.total;
+    const size_t need = storing ? body_stored_bwd_bytes(bd, g0) : bw.total;
     if (int rc = check_ws(ws, ws_bytes, need)) return rc;
     for (int s = 0; s < bd.stages; ++s)
         if (overlaps_range(&tops[s], ws, need) || overlaps_range(&dtops[s], ws, need))
             return fail(RVN_ERR_ALIAS, "tops[%d] or dtops[%d] overlaps the workspace", s, s);
+    if (storing) {
+        const size_t store_need = body_store_at(bd, g0, bd.stages);
+        if (int rc = check_store("store", store, store_bytes, store_need)) return rc;
+        if (ranges_overlap(store, store_need, ws, need)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
+        for (int s = 0; s < bd.stages; ++s)
+            if (overlaps_range(&tops[s], store, store_need) || overlaps_range(&dtops[s], store, store_need))
+                return fail(RVN_ERR_ALIAS, "tops[%d] or dtops[%d] overlaps the store", s, s);
+    }
     Ctx cx;
     cx.stream = static_cast<hipStream_t>(hip_stream);
     const bool acc = accumulate_wgrads != 0;
@@ -586,6 +621,11 @@ int body_bwd_impl(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_t
         const Plan pl = make_plan(bd.stage[s], g, true, frac_bits != 0);
         const View t1 = half_view(&tops[s], 0), t2 = half_view(&tops[s], 1);
         const View d1 = half_view(&dtops[s], 0), d2 = half_view(&dtops[s], 1);
+        if (storing) {
+            stack_backward_stored(cx, bd.stage[s], bd.depth[s], pl, bind(pl, ws), g, d1, d2, stage_params[s], d1, d2, stage_grads[s], acc,
+                                  static_cast<const char *>(store) + body_store_at(bd, g0, s), ws);
+            continue;
+        }
         stack_backward(cx, bd.stage[s], bd.depth[s], pl, bind(pl, ws), g, t1, t2, d1, d2, stage_params[s], t1, t2, d1, d2,
                        stage_grads[s], acc, frac_bits);
     }
@@ -609,6 +649,30 @@ int revnet_body_bwd_fixed(const rvn_body_desc *desc, int32_t frac_bits, const rv
     if (frac_bits < 1 || frac_bits > 30) return fail(RVN_ERR_SHAPE, "frac_bits = %d out of range [1, 30]", frac_bits);
     return body_bwd_impl(desc, tops, dtops, stage_params, down_params, stage_grads, down_grads, accumulate_wgrads, ws,
                          ws_bytes, hip_stream, frac_bits);
+}
+
+int revnet_body_stored_bytes(const rvn_body_desc *desc, int64_t n, int64_t h, int64_t w, size_t *store_bytes, size_t *fwd_ws_bytes,
+                             size_t *bwd_ws_bytes) {
+    if (int rc = check_body_desc(desc, n, h, w)) return rc;
+    const Geo g{(int)n, (int)h, (int)w};
+    if (store_bytes) *store_bytes = body_store_at(*desc, g, desc->stages);
+    if (fwd_ws_bytes) *fwd_ws_bytes = body_ws_bytes(*desc, g, false);
+    if (bwd_ws_bytes) *bwd_ws_bytes = body_stored_bwd_bytes(*desc, g);
+    return RVN_OK;
+}
+
+int revnet_body_fwd_stored(const rvn_body_desc *desc, const rvn_tensor *x, const rvn_block_params *const *stage_params,
+                           const rvn_down_params *down_params, const rvn_tensor *tops, void *store, size_t store_bytes, void *ws,
+                           size_t ws_bytes, void *hip_stream) {
+    return body_fwd_impl(desc, x, stage_params, down_params, tops, ws, ws_bytes, hip_stream, 0, true, store, store_bytes);
+}
+
+int revnet_body_bwd_stored(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_tensor *dtops,
+                           const rvn_block_params *const *stage_params, const rvn_down_params *down_params,
+                           const rvn_block_grads *const *stage_grads, const rvn_down_grads *down_grads, int accumulate_wgrads,
+                           const void *store, size_t store_bytes, void *ws, size_t ws_bytes, void *hip_stream) {
+    return body_bwd_impl(desc, tops, dtops, stage_params, down_params, stage_grads, down_grads, accumulate_wgrads, ws, ws_bytes,
+                         hip_stream, 0, true, store, store_bytes);
 }
 
 int revnet_body_fixed_workspace_bytes(const rvn_body_desc *desc, int64_t n, int64_t h, int64_t w, size_t *fwd_bytes,

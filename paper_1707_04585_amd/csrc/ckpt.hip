@@ -1,0 +1,358 @@
+// Activation checkpoints in 8 bits: save, load, and the backward pass of BN + ReLU straight from the codes.
+//
+// A plane's pixels fall into groups of 128 that share a scale (see include/revnet.h for the format).  Everything here
+// is a few instructions on every element of a tensor that is read or written once: bound by memory, save at 5 bytes an
+// element (4 in, 1 out), load at 5, the backward pass at 9 (13 with a skip tensor) where a channel fits one workgroup's
+// registers and 14 (18) where the sums take a launch of their own.
+//
+// A lane works on four neighbouring pixels (quads.h): 16 bytes of fp32, 4 of codes.  Planes of any size and tensors of
+// any alignment take the same path.
+#include "fast_div.h"
+#include "kernels.h"
+#include "quads.h"
+#include "wgrad_reduce.h"
+
+namespace rvn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr float kTop = 126.f;                          // the largest code that rounding alone gives
+constexpr float kLeast = 126.f * 1.17549435e-38f;      // smallest group magnitude: keeps the scale a normal number
+
+typedef uint32_t u32_any __attribute__((aligned(1)));
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+typedef u16x4 u16x4_any __attribute__((aligned(2)));
+
+__device__ __forceinline__ uint32_t load_codes(const int8_t *p, int left) {
+    if (left >= 4) return *reinterpret_cast<const u32_any *>(p);
+    uint32_t v = (uint8_t)p[0];
+    if (left > 1) v |= (uint32_t)(uint8_t)p[1] << 8;
+    if (left > 2) v |= (uint32_t)(uint8_t)p[2] << 16;
+    return v;
+}
+__device__ __forceinline__ f4 decode(uint32_t q, float s) {
+    f4 v;
+    v.x = (float)(int8_t)q * s;
+    v.y = (float)(int8_t)(q >> 8) * s;
+    v.z = (float)(int8_t)(q >> 16) * s;
+    v.w = (float)((int32_t)q >> 24) * s;
+    return v;
+}
+
+// 2^tshift neighbouring lanes share a group (128 pixels, or a whole smaller plane); blockIdx.x counts the groups of an
+// image, blockIdx.y the images.
+template <bool BN>
+__global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict__ x, int64_t sn, int64_t sc, int N, int C, int HW,
+                                                        int G, FastDiv by_g, int tshift, const float *__restrict__ stats,
+                                                        int8_t *__restrict__ q, float *__restrict__ s) {
+    const int item = (int)blockIdx.x * (kThreads >> tshift) + ((int)threadIdx.x >> tshift), lane = (int)threadIdx.x & ((1 << tshift) - 1);
+    const bool live = item < C * G;
+    const int ch = live ? quotient(item, by_g) : 0, group = live ? item - ch * G : 0;
+    const int i = group * kCkptGroup + lane * 4, left = HW - i;
+    const bool mine = live && left > 0;
+    float scale = 0.f, shift = 0.f;
+    if (BN) scale = stats[2 * C + ch], shift = stats[3 * C + ch];
+    for (int n = (int)blockIdx.y; n < N; n += (int)gridDim.y) {
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        if (mine) v = load4(x + (int64_t)n * sn + (int64_t)ch * sc + i, left);
+        // magnitudes as bit patterns: these order as the values do, infinities and NaN on top
+        uint32_t most = max(max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu),
+                            max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu));
+        for (int o = 1 << tshift >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+        if (!mine) continue;
+        const bool finite = most < 0x7f800000u;
+        const float a = fmaxf(finite ? __uint_as_float(most) : 1.f, kLeast);
+        const float step = a / kTop, inverse = kTop / a;
+        uint32_t word = 0;
+        if (finite) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float c = rintf(v[j] * inverse);
+                if (BN) {
+                    const bool want = fmaf(v[j], scale, shift) > 0.f, got = fmaf(c * step, scale, shift) > 0.f;
+                    if (want != got) c += (scale > 0.f) == want ? 1.f : -1.f;
+                }
+                word |= ((uint32_t)(int)c & 0xffu) << (8 * j);
+            }
+        }
+        const int64_t plane = (int64_t)n * C + ch;
+        int8_t *out = q + plane * HW + i;
+        if (left >= 4) {
+            *reinterpret_cast<u32_any *>(out) = word;
+        } else {
+            for (int j = 0; j < left; ++j) out[j] = (int8_t)(word >> (8 * j));
+        }
+        if (lane == 0) s[plane * G + group] = finite ? step : __uint_as_float(0x7fc00000u);
+    }
+}
+
+// One lane per four pixels; blockIdx.x counts the quads of an image, blockIdx.y the images.
+__global__ __launch_bounds__(kThreads) void ckpt_load_k(const int8_t *__restrict__ q, const float *__restrict__ s, int N, int C, int HW,
+                                                        int G, FastDiv by_per, float *__restrict__ x, int64_t sn, int64_t sc) {
+    const int per = (int)by_per.d, item = (int)blockIdx.x * kThreads + (int)threadIdx.x;
+    if (item >= C * per) return;
+    const int ch = quotient(item, by_per), i = (item - ch * per) * 4, left = HW - i;
+    for (int n = (int)blockIdx.y; n < N; n += (int)gridDim.y) {
+        const int64_t plane = (int64_t)n * C + ch;
+        const uint32_t word = load_codes(q + plane * HW + i, left);
+        store4(x + (int64_t)n * sn + (int64_t)ch * sc + i, left, decode(word, s[plane * G + i / kCkptGroup]));
+    }
+}
+
+// ---- backward pass of BN + ReLU ----------------------------------------------------------------------------
+
+struct BnLayer {
+    const int8_t *q;
+    const float *s, *stats;
+    int N, C, HW, G;
+    FastDiv by_per;  // quads of a plane
+};
+
+// dz and xh of one quad of channel ch (pixels beyond the plane's end: zero)
+__device__ __forceinline__ void quad(const BnLayer &b, uint32_t word, float step, f4 da, int left, float mean, float rstd, float scale,
+                                     float shift, f4 &dz, f4 &xh) {
+    const f4 v = decode(word, step);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        dz[j] = j < left && fmaf(v[j], scale, shift) > 0.f ? da[j] : 0.f;
+        xh[j] = (v[j] - mean) * rstd;
+    }
+}
+
+__device__ __forceinline__ void put_quad(f4 r, int left, float *po, uint16_t *p16) {
+    if (p16) {  // dense bf16, nearest even: what the convolutions that read it would round it to
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        const u16x4 h = __builtin_bit_cast(u16x4, __builtin_convertvector(r, bf16x4));
+        if (left >= 4) {
+            *reinterpret_cast<u16x4_any *>(p16) = h;
+        } else {
+            for (int j = 0; j < left; ++j) p16[j] = h[j];
+        }
+    } else {
+        store4(po, left, r);
+    }
+}
+
+// sums[ch][split] = (sum dz, sum dz * xh) over a share of a channel's quads; threads add in fp32 (at most a few hundred
+// terms each), everything above in double
+__global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, int share,
+                                                             double2 *sums) {
+    __shared__ double part[4][2];
+    const int ch = (int)blockIdx.y, per = (int)b.by_per.d, total = b.N * per;
+    const int first = (int)blockIdx.x * share, last = min(total, first + share);
+    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
+    float a0 = 0.f, a1 = 0.f;
+    for (int e = first + (int)threadIdx.x; e < last; e += kThreads) {
+        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
+        const int64_t plane = (int64_t)n * b.C + ch;
+        const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
+        const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
+        f4 dz, xh;
+        quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz, xh);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            a0 += dz[j];
+            a1 = fmaf(dz[j], xh[j], a1);
+        }
+    }
+    const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = t0, part[threadIdx.x >> 6][1] = t1;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        sums[(int64_t)ch * gridDim.x + blockIdx.x] =
+            make_double2((part[0][0] + part[1][0]) + (part[2][0] + part[3][0]), (part[0][1] + part[1][1]) + (part[2][1] + part[3][1]));
+}
+
+__device__ __forceinline__ void put_sums(double sb, double sg, float *dgamma, float *dbeta, int ch, int accumulate) {
+    dbeta[ch] = (accumulate ? dbeta[ch] : 0.f) + (float)sb;
+    dgamma[ch] = (accumulate ? dgamma[ch] : 0.f) + (float)sg;
+}
+
+constexpr int kApplyQuads = 4;  // a thread of the apply pass
+
+// The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
+template <bool SKIP>
+__global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc,
+                                                            const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_chunks,
+                                                            float *dgamma, float *dbeta, int accumulate, const float *skip, int64_t ksn,
+                                                            int64_t ksc, float *out, int64_t osn, int64_t osc, uint16_t *out16,
+                                                            const WgradReduce carry) {
+    if ((int)blockIdx.x < carry.blocks) {
+        __shared__ float lds[kThreads];
+        wgrad_reduce_body(carry, (int)blockIdx.x, lds);
+        return;
+    }
+    const int bx = (int)blockIdx.x - carry.blocks, ch = quotient(bx, by_chunks), chunk = bx - ch * (int)by_chunks.d;
+    const int per = (int)b.by_per.d, total = b.N * per;
+    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
+    // every wavefront adds the channel's partial sums for itself, in the same order
+    const int lane = (int)threadIdx.x & 63;
+    double2 p = make_double2(0.0, 0.0);
+    if (lane < S) p = sums[(int64_t)ch * S + lane];
+    const double sb = wave_total(p.x), sg = wave_total(p.y);
+    if (chunk == 0 && threadIdx.x == 0) put_sums(sb, sg, dgamma, dbeta, ch, accumulate);
+    const float c1 = (float)(sb * inv_m), c2 = (float)(sg * inv_m);
+#pragma unroll
+    for (int k = 0; k < kApplyQuads; ++k) {
+        const int e = (chunk * kApplyQuads + k) * kThreads + (int)threadIdx.x;
+        if (e >= total) return;
+        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
+        const int64_t plane = (int64_t)n * b.C + ch;
+        const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
+        const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
+        f4 dz, xh, kv = {0.f, 0.f, 0.f, 0.f};
+        if (SKIP) kv = load4(skip + (int64_t)n * ksn + (int64_t)ch * ksc + i, left);
+        quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz, xh);
+        f4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            r[j] = scale * ((dz[j] - c1) - xh[j] * c2);
+            if (SKIP) r[j] += kv[j];
+        }
+        put_quad(r, left, out + (int64_t)n * osn + (int64_t)ch * osc + i, out16 ? out16 + plane * b.HW + i : nullptr);
+    }
+}
+
+// Both passes in one launch where a channel's quads fit the registers of one workgroup: codes and da are read once.
+constexpr int kFusedQuads = 8;
+
+template <int T, bool SKIP>
+__global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, double inv_m,
+                                                     float *dgamma, float *dbeta, int accumulate, const float *skip, int64_t ksn,
+                                                     int64_t ksc, float *out, int64_t osn, int64_t osc, uint16_t *out16,
+                                                     const WgradReduce carry) {
+    if constexpr (T == kThreads) {
+        if ((int)blockIdx.x < carry.blocks) {
+            __shared__ float lds[kThreads];
+            wgrad_reduce_body(carry, (int)blockIdx.x, lds);
+            return;
+        }
+    }
+    __shared__ double part[T / 64][2];
+    const int ch = (int)blockIdx.x - carry.blocks, per = (int)b.by_per.d, total = b.N * per;
+    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
+    f4 dz[kFusedQuads], xh[kFusedQuads];
+    float a0 = 0.f, a1 = 0.f;
+#pragma unroll
+    for (int k = 0; k < kFusedQuads; ++k) {
+        const int e = (int)threadIdx.x + k * T;
+        dz[k] = f4{0.f, 0.f, 0.f, 0.f};
+        xh[k] = dz[k];
+        if (e < total) {
+            const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
+            const int64_t plane = (int64_t)n * b.C + ch;
+            const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
+            const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
+            quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz[k], xh[k]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            a0 += dz[k][j];
+            a1 = fmaf(dz[k][j], xh[k][j], a1);
+        }
+    }
+    const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = t0, part[threadIdx.x >> 6][1] = t1;
+    __syncthreads();
+    double sb = 0.0, sg = 0.0;
+#pragma unroll
+    for (int w = 0; w < T / 64; ++w) sb += part[w][0], sg += part[w][1];
+    if (threadIdx.x == 0) put_sums(sb, sg, dgamma, dbeta, ch, accumulate);
+    const float c1 = (float)(sb * inv_m), c2 = (float)(sg * inv_m);
+#pragma unroll
+    for (int k = 0; k < kFusedQuads; ++k) {
+        const int e = (int)threadIdx.x + k * T;
+        if (e >= total) return;
+        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
+        f4 r;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = scale * ((dz[k][j] - c1) - xh[k][j] * c2);
+        if (SKIP) r += load4(skip + (int64_t)n * ksn + (int64_t)ch * ksc + i, left);
+        put_quad(r, left, out + (int64_t)n * osn + (int64_t)ch * osc + i, out16 ? out16 + ((int64_t)n * b.C + ch) * b.HW + i : nullptr);
+    }
+}
+
+unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per); }
+
+// Workgroups a channel's sums are split over: enough to fill the chip, at most one partial sum per lane.
+int ckpt_bn_splits(int c, const Geo &g) {
+    const int64_t quads = (int64_t)g.n * quads_of(g.hw());
+    int64_t s = c >= 2048 ? 1 : 2048 / c;
+    s = s < 64 ? s : 64;
+    const int64_t most = (quads + 2 * kThreads - 1) / (2 * kThreads);
+    return (int)(s < most ? s : most);
+}
+
+}  // namespace
+
+void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k) {
+    const int hw = g.hw(), G = ckpt_groups(hw);
+    const double planes = (double)g.n * c;
+    if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
+    int tshift = 0;  // lanes of a group: 32, or as many as a smaller plane has quads, rounded up to a power of two
+    while (tshift < 5 && (4 << tshift) < hw) ++tshift;
+    const dim3 grid(blocks_for((int64_t)c * G, kThreads >> tshift), (unsigned)(g.n < 65535 ? g.n : 65535));
+    if (stats)
+        cx.run(ckpt_save_k<true>, grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
+    else
+        cx.run(ckpt_save_k<false>, grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
+}
+
+void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out) {
+    const int hw = g.hw(), G = ckpt_groups(hw), per = quads_of(hw);
+    const double planes = (double)g.n * c;
+    if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
+    const dim3 grid(blocks_for((int64_t)c * per, kThreads), (unsigned)(g.n < 65535 ? g.n : 65535));
+    cx.run(ckpt_load_k, grid, dim3(kThreads), 0, k.q, k.s, g.n, c, hw, G, fast_div(per), out.p, out.sn, out.sc);
+}
+
+size_t ckpt_bn_scratch_floats(int c, const Geo &g) { return (size_t)c * ckpt_bn_splits(c, g) * 4; }
+
+void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats, float *scratch, float *dgamma, float *dbeta,
+                      bool accumulate, const View *skip, View out, const WgradReduce *carry, uint16_t *out16) {
+    if (out16 && skip) {  // a caller's mistake: nothing sensible to launch
+        cx.fail(hipErrorInvalidValue);
+        return;
+    }
+    const int hw = g.hw(), per = quads_of(hw), total = g.n * per;
+    const double elems = (double)g.pixels() * c;
+    const BnLayer b{k.q, k.s, stats, g.n, c, hw, ckpt_groups(hw), fast_div(per)};
+    const double inv_m = 1.0 / (double)g.pixels();
+    WgradReduce red{};
+    if (carry) red = *carry;
+    if (red.blocks < 0) red.blocks = 0;
+    const View kv = skip ? *skip : View{nullptr, 0, 0};
+    const int acc = accumulate ? 1 : 0;
+    const double out_bytes = out16 ? 2.0 : skip ? 8.0 : 4.0;
+    const bool wide = total > kFusedQuads * kThreads;
+    if (total <= kFusedQuads * 1024 && !(wide && (red.blocks > 0 || c < 256))) {
+        if (!cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) return;
+        const dim3 grid((unsigned)(c + red.blocks));
+#define RVN_FUSED(T, K)                                                                                                          \
+    cx.run(ckpt_bn_fused_k<T, K>, grid, dim3(T), 0, b, da.p, da.sn, da.sc, inv_m, dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p, \
+           out.sn, out.sc, out16, red)
+        if (wide && skip) RVN_FUSED(1024, true);
+        else if (wide) RVN_FUSED(1024, false);
+        else if (skip) RVN_FUSED(kThreads, true);
+        else RVN_FUSED(kThreads, false);
+#undef RVN_FUSED
+        return;
+    }
+    const int S = ckpt_bn_splits(c, g), share = (total + S - 1) / S;
+    double2 *sums = reinterpret_cast<double2 *>(scratch);
+    if (cx.launch(K_BN_BWD_REDUCE, 5.0 * elems))
+        cx.run(ckpt_bn_reduce_k, dim3((unsigned)S, (unsigned)c), dim3(kThreads), 0, b, da.p, da.sn, da.sc, share, sums);
+    if (cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) {
+        const int chunks = (total + kApplyQuads * kThreads - 1) / (kApplyQuads * kThreads);
+        const dim3 grid((unsigned)(chunks * c + red.blocks));
+        if (skip)
+            cx.run(ckpt_bn_apply_k<true>, grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta,
+                   acc, kv.p, kv.sn, kv.sc, out.p, out.sn, out.sc, out16, red);
+        else
+            cx.run(ckpt_bn_apply_k<false>, grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta,
+                   acc, kv.p, kv.sn, kv.sc, out.p, out.sn, out.sc, out16, red);
+    }
+}
+
+}  // namespace rvn

@@ -49,6 +49,9 @@ enum KernelId {
     K_FIXED_POINT,
     K_STEM,
     K_SPLITK_REDUCE,  // second launch of a convolution whose input channels were split over workgroups
+    K_CKPT,
+    K_HEAD,
+    K_LOGPROB,
     K_COUNT
 };
 const char *kernel_name(int id);
@@ -391,6 +394,56 @@ void fix_to_float(Ctx &cx, View x, int c, Geo g, int frac_bits, float *out);
 void fix_axpy(Ctx &cx, View r, const float *f, int c, Geo g, int frac_bits, int sign, View out);
 // out (int32 codes) = rint(x * 2^frac_bits).
 void fix_from_float(Ctx &cx, View x, int c, Geo g, int frac_bits, View out);
+
+// ---- activation checkpoints in 8 bits (ckpt.hip) ------------------------------
+// Codes [n][c][hw] and scales [n][c][ckpt_groups(hw)], both dense.
+struct Ckpt {
+    int8_t *q;
+    float *s;
+};
+constexpr int kCkptGroup = RVN_CKPT_GROUP;
+inline int ckpt_groups(int hw) { return (hw + kCkptGroup - 1) / kCkptGroup; }
+// stats: null, or the four statistics arrays of the BN layer that reads x, whose ReLU decisions are then kept.
+void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k);
+void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out);
+// bn_relu_bwd with x read from a checkpoint and da anywhere; scratch: ckpt_bn_scratch_floats(c, g) floats.  `carry`, out16: as there
+// (out16 needs no alignment here; no skip).
+size_t ckpt_bn_scratch_floats(int c, const Geo &g);
+void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats, float *scratch, float *dgamma, float *dbeta,
+                      bool accumulate, const View *skip, View out, const WgradReduce *carry = nullptr, uint16_t *out16 = nullptr);
+
+// ---- classification head (head.hip) --------------------------------------------
+// What the forward pass leaves for the backward pass: the statistics of x, and for every plane the mean of
+// ReLU(BN(x)), how many pixels are positive and the sum of their xhat ([n][c] each).
+struct HeadSaved {
+    float *stats, *pooled, *count, *xhat;
+};
+void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, const float *beta, HeadSaved s);
+// logits[n][k] = pooled[n][:] . w[k][:] + b[k]
+void head_linear(Ctx &cx, const float *pooled, int n, int c, int classes, const float *w, const float *b, float *logits, int64_t ld);
+// d_pooled[n][c] = dl . w, dw[k][c] (+)= dl^T . pooled, db[k] (+)= sums of dl: one launch
+void head_linear_bwd(Ctx &cx, const float *dl, int64_t ld, const float *pooled, int n, int c, int classes, const float *w,
+                     float *d_pooled, float *dw, float *db, bool accumulate);
+void head_pool_bwd(Ctx &cx, View x, int c, Geo g, HeadSaved s, const float *d_pooled, float *dgamma, float *dbeta, bool accumulate,
+                   View dx);
+
+// ---- log probabilities of labels (logprob.hip) -----------------------------------
+struct Logits {
+    const void *p;
+    bool bf16;
+    int64_t rows, ld;
+    int classes;
+};
+struct LogprobOut {
+    float *logprob, *entropy, *lse;
+    int64_t *top_ids;
+    float *top_logprob;
+    int top_k;
+};
+size_t logprob_scratch_bytes(int64_t rows, int classes, int top_k);
+void logprob_fwd(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch);
+void logprob_bwd(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,
+                 const float *d_entropy, float scale, void *out, int64_t out_ld);
 
 // ---- stem: image convolution and max-pooling ahead of the reversible stages ----
 // Direct fp32 kernels for a convolution whose input has a handful of channels

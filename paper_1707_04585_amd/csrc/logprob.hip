@@ -1,0 +1,485 @@
+// Log probabilities of labels under a row's softmax, with entropy, normaliser and the most likely classes, in one pass
+// over the logits; and their gradient.  Bound by memory: the forward pass reads every logit once (a row's top classes
+// cost reads of the few vectors that can hold them), the gradient reads and writes every logit once.
+//
+// Forward.  A thread keeps, over the vectors of 16 bytes that it reads, the largest value m so far, s = sum 2^((x-m) L) and
+// t = sum 2^((x-m) L) (x-m) L with L = log2(e), and rescales s and t when m grows; joining two such triples is the same
+// step, so that threads, wavefronts and workgroups of a row join theirs in a fixed order.  With the total
+//     lse = m + ln s,   logprob = (x_label - m) - ln s,   entropy = ln s - ln 2 * t / s.
+// The sums are fp32: at most a few hundred terms in a thread, then a tree.
+//
+// Top classes.  Classes are ordered by one 64-bit key: the value's bits made monotonic, above the complement of the class
+// number, so that no two are equal.  A thread knows the largest key of its own vectors; a wavefront takes the largest
+// among its threads, and only the one thread that gave it looks for its next smaller key, for which the whole wavefront
+// reads that thread's vectors (at most one vector a lane for rows up to 64 * 64 vectors per wavefront).  Each wavefront lists
+// its first top_k this way, and the lists are merged.
+#include "kernels.h"
+
+namespace rvn {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kFly = 4;  // vectors a thread requests before it uses the first
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr float kLowest = -3.402823466e38f;
+
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef u4 u4_any __attribute__((aligned(2)));
+
+template <typename T>
+struct Vec;  // 16 bytes of a row as fp32 values, and back
+template <>
+struct Vec<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ float one(const void *p, int64_t i) { return static_cast<const float *>(p)[i]; }
+    static __device__ __forceinline__ void widen(u4 w, float (&v)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = __uint_as_float(w[e]);
+    }
+    static __device__ __forceinline__ u4 narrow(const float (&v)[E]) {
+        return u4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+    }
+    static __device__ __forceinline__ void put(void *p, int64_t i, float v) { static_cast<float *>(p)[i] = v; }
+};
+struct Bf16 {
+    uint16_t bits;
+};
+template <>
+struct Vec<Bf16> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ float one(const void *p, int64_t i) {
+        return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
+    }
+    static __device__ __forceinline__ void widen(u4 w, float (&v)[E]) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ uint32_t pair(float lo, float hi) {
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const f2 v = {lo, hi};
+        return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));  // nearest even
+    }
+    static __device__ __forceinline__ u4 narrow(const float (&v)[E]) {
+        return u4{pair(v[0], v[1]), pair(v[2], v[3]), pair(v[4], v[5]), pair(v[6], v[7])};
+    }
+    static __device__ __forceinline__ void put(void *p, int64_t i, float v) {
+        static_cast<uint16_t *>(p)[i] = (uint16_t)pair(v, 0.f);
+    }
+};
+
+// The vector that starts at class `at` of a row of `classes` > at; what lies behind the row reads as -infinity.
+template <typename T>
+__device__ __forceinline__ void load_vec(const T *row, int at, int classes, float (&v)[Vec<T>::E]) {
+    constexpr int E = Vec<T>::E;
+    if (at + E <= classes) {
+        Vec<T>::widen(*reinterpret_cast<const u4_any *>(row + at), v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = at + e < classes ? Vec<T>::one(row, at + e) : -INFINITY;
+    }
+}
+
+// Bits that order as the values do, -0 as 0, NaN above all; never 0, and never 0xffffffff, which is above every key.
+constexpr uint32_t kNanOrder = 0xff800001u;
+__device__ __forceinline__ uint32_t order_bits(float x) {
+    if (x != x) return kNanOrder;
+    const uint32_t b = __float_as_uint(x + 0.f);
+    return b ^ ((int32_t)b < 0 ? 0xffffffffu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t order) {
+    if (order == kNanOrder) return __uint_as_float(0x7fc00000u);
+    return __uint_as_float(order ^ ((int32_t)order < 0 ? 0x80000000u : 0xffffffffu));
+}
+
+__device__ __forceinline__ uint32_t wave_most(uint32_t v) {  // over the 64 lanes, all of them active
+#define RVN_STEP(ctrl, rows) v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xf, false))
+    RVN_STEP(0x111, 0xf);  // row_shr 1, 2, 4, 8: the last lane of each row of 16 has the row's
+    RVN_STEP(0x112, 0xf);
+    RVN_STEP(0x114, 0xf);
+    RVN_STEP(0x118, 0xf);
+    RVN_STEP(0x142, 0xa);  // row_bcast 15 and 31: lane 63 has all
+    RVN_STEP(0x143, 0xc);
+#undef RVN_STEP
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
+
+struct Key {
+    uint32_t hi, lo;  // order bits; complement of the class number.  {0, 0}: none
+};
+__device__ __forceinline__ bool less(Key a, Key b) { return a.hi < b.hi || (a.hi == b.hi && a.lo < b.lo); }
+__device__ __forceinline__ Key wave_most(Key k) {
+    const uint32_t hi = wave_most(k.hi);
+    return Key{hi, wave_most(k.hi == hi ? k.lo : 0u)};
+}
+
+struct Sums {
+    float m, s, t;
+};
+__device__ __forceinline__ Sums join(Sums a, Sums b) {
+    const float m = fmaxf(a.m, b.m);
+    const float da = (a.m - m) * kLog2e, db = (b.m - m) * kLog2e;
+    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
+    // (differences below -200 have a factor of 0: clamped, so that 0 * -infinity cannot arise)
+    return Sums{m, a.s * fa + b.s * fb, fa * (a.t + a.s * fmaxf(da, -200.f)) + fb * (b.t + b.s * fmaxf(db, -200.f))};
+}
+__device__ __forceinline__ Sums wave_join(Sums v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v = join(v, Sums{__shfl_xor(v.m, o, 64), __shfl_xor(v.s, o, 64), __shfl_xor(v.t, o, 64)});
+    return v;
+}
+
+// A team of NT threads on classes [first, last) of a row: vector v of that part belongs to thread v % NT.
+template <typename T>
+struct Part {
+    const T *row;  // at class `first`
+    int first, length, vecs, NT;
+};
+
+template <typename T>
+__device__ __forceinline__ Key best_below(const Part<T> &p, int v, Key below, Key best) {
+    constexpr int E = Vec<T>::E;
+    float x[E];
+    load_vec(p.row, v * E, p.length, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const Key k{order_bits(x[e]), 0xffffffffu - (uint32_t)(p.first + v * E + e)};
+        if (v * E + e < p.length && less(k, below) && less(best, k)) best = k;
+    }
+    return best;
+}
+
+template <typename T>
+__device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T>::E], float most) {
+    constexpr int E = Vec<T>::E;
+    const float m = fmaxf(a.m, most);
+    const float down = (a.m - m) * kLog2e, f = __builtin_amdgcn_exp2f(down);
+    a.t = f * (a.t + a.s * fmaxf(down, -200.f));
+    a.s *= f;
+    a.m = m;
+#pragma unroll
+    for (int u = 0; u < kFly; ++u)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float d = (x[u][e] - m) * kLog2e, w = __builtin_amdgcn_exp2f(d);
+            a.s += w;
+            a.t = fmaf(w, fmaxf(d, -200.f), a.t);  // (a NaN stays one in w)
+        }
+}
+
+// The sums of a thread's vectors, and where its largest value is: the first group of kFly vectors that holds it.
+template <typename T>
+__device__ __forceinline__ Sums stream(const Part<T> &p, int thread, float &top, int &top_group) {
+    constexpr int E = Vec<T>::E;
+    Sums a{kLowest, 0.f, 0.f};
+    top = -INFINITY;
+    top_group = 0;
+    for (int g = 0; thread + g * kFly * p.NT < p.vecs; ++g) {
+        float x[kFly][E];
+        const int v0 = thread + g * kFly * p.NT;
+        if ((v0 + (kFly - 1) * p.NT) * E + E <= p.length) {
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) Vec<T>::widen(*reinterpret_cast<const u4_any *>(p.row + (v0 + u * p.NT) * E), x[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {
+                if (v0 + u * p.NT < p.vecs) {
+                    load_vec(p.row, (v0 + u * p.NT) * E, p.length, x[u]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) x[u][e] = -INFINITY;
+                }
+            }
+        }
+        float most = x[0][0];
+#pragma unroll
+        for (int u = 0; u < kFly; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) most = fmaxf(most, x[u][e]);
+        if (most > top) {
+            top = most;
+            top_group = g;
+        }
+        add_values<T>(a, x, most);
+    }
+    return a;
+}
+
+// list[0 .. top_k) = the largest keys of the vectors of one wavefront's threads in falling order, then {0, 0}.  Every
+// lane of the wavefront is active.  nan: the part holds one (no thread's `top` counts it).
+template <typename T>
+__device__ __forceinline__ void wave_top(const Part<T> &p, int thread, float top, int top_group, bool nan, int top_k, Key *list) {
+    const int lane = thread & 63;
+    const Key above{0xffffffffu, 0xffffffffu};
+    Key mine{0u, 0u};
+    const int g0 = nan ? 0 : top_group, g1 = nan ? (p.vecs + kFly * p.NT - 1) / (kFly * p.NT) : top_group + 1;
+    for (int g = g0; g < g1; ++g)
+        for (int u = 0; u < kFly; ++u) {
+            const int v = thread + (g * kFly + u) * p.NT;
+            if (v < p.vecs) mine = best_below(p, v, above, mine);
+        }
+    for (int r = 0; r < top_k; ++r) {
+        const Key most = wave_most(mine);
+        if (lane == 0) list[r] = most;
+        if (most.hi == 0u) {  // (uniform) nothing left
+            if (lane > r && lane < top_k) list[lane] = Key{0u, 0u};
+            return;
+        }
+        if (r + 1 == top_k) return;
+        const int winner = __ffsll((unsigned long long)__ballot(mine.hi == most.hi && mine.lo == most.lo)) - 1;
+        Key next{0u, 0u};
+        for (int v = (thread - lane) + winner + lane * p.NT; v < p.vecs; v += 64 * p.NT) next = best_below(p, v, most, next);
+        next = wave_most(next);
+        if (lane == winner) mine = next;
+    }
+}
+
+// Merges `lists` <= 64 falling lists of top_k keys; `emit(r, key)` is called by lane 0 for the r-th largest.
+template <typename Emit>
+__device__ __forceinline__ void merge_lists(const Key *keys, int lists, int top_k, int lane, Emit emit) {
+    int at = 0;
+    Key mine = lane < lists ? keys[lane * top_k] : Key{0u, 0u};
+    for (int r = 0; r < top_k; ++r) {
+        const Key most = wave_most(mine);
+        if (lane == 0) emit(r, most);
+        if (mine.hi == most.hi && mine.lo == most.lo && most.hi != 0u) {
+            ++at;
+            mine = at < top_k ? keys[lane * top_k + at] : Key{0u, 0u};
+        }
+    }
+}
+
+// One lane writes a row's results.
+struct Row {
+    float m, log_s;
+    bool nan, empty;
+};
+__device__ __forceinline__ Row row_of(Sums a) { return Row{a.m, logf(a.s), !(a.s >= 0.f), a.s == 0.f}; }
+
+__device__ __forceinline__ float log_probability(const Row &r, float x) {
+    return r.nan ? __uint_as_float(0x7fc00000u) : r.empty ? -INFINITY : (x - r.m) - r.log_s;
+}
+
+template <typename T>
+__device__ __forceinline__ void put_row(const T *row, int classes, int64_t at, Sums a, const int64_t *labels, const LogprobOut &out) {
+    const Row r = row_of(a);
+    if (out.logprob) {
+        const int64_t label = labels[at];
+        float v = __uint_as_float(0x7fc00000u);
+        if (label == RVN_NO_LABEL) v = 0.f;
+        else if (label >= 0 && label < classes) v = log_probability(r, Vec<T>::one(row, label));
+        out.logprob[at] = v;
+    }
+    if (out.entropy) out.entropy[at] = r.empty ? 0.f : r.log_s - kLn2 * (a.t / a.s);
+    if (out.lse) out.lse[at] = r.nan ? __uint_as_float(0x7fc00000u) : a.m + r.log_s;
+}
+
+__device__ __forceinline__ void put_top(const LogprobOut &out, int64_t at, int r, Key k, const Row &row) {
+    out.top_ids[at * out.top_k + r] = (int64_t)(0xffffffffu - k.lo);
+    if (out.top_logprob) out.top_logprob[at * out.top_k + r] = log_probability(row, value_of(k.hi));
+}
+
+// One wavefront per row, for short rows; four rows to a workgroup.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t rows, int64_t ld, int classes, const int64_t *labels,
+                                                           const LogprobOut out) {
+    __shared__ Key lists[kThreads / 64][RVN_MAX_TOP_K];
+    const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+    const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + wave;
+    if (at >= rows) return;
+    const Part<T> p{x + at * ld, 0, classes, (classes + Vec<T>::E - 1) / Vec<T>::E, 64};
+    float top;
+    int top_group;
+    const Sums a = wave_join(stream(p, lane, top, top_group));
+    if (lane == 0) put_row(p.row, classes, at, a, labels, out);
+    if (out.top_k == 0) return;
+    wave_top(p, lane, top, top_group, !(a.s >= 0.f), out.top_k, lists[wave]);
+    __builtin_amdgcn_wave_barrier();
+    const Row row = row_of(a);
+    if (lane < out.top_k) put_top(out, at, lane, lists[wave][lane], row);
+}
+
+// A workgroup of NW wavefronts per part of a row.  splits == 1: the whole row, results written here.  Otherwise the
+// part's sums and list go to `sums` and `keys` ([row][split]) for logprob_join_k.
+template <typename T, int NW>
+__global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t ld, int classes, int splits, int share,
+                                                           const int64_t *labels, const LogprobOut out, float4 *sums, Key *keys) {
+    __shared__ Key lists[NW * RVN_MAX_TOP_K];
+    __shared__ Sums parts[NW];
+    const int thread = (int)threadIdx.x, wave = thread >> 6, lane = thread & 63;
+    const int64_t at = splits == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)splits);
+    const int split = splits == 1 ? 0 : (int)(blockIdx.x - (unsigned)at * (unsigned)splits);
+    const int first = split * share, length = min(share, classes - first);
+    const T *row = x + at * ld;
+    const Part<T> p{row + first, first, length, (length + Vec<T>::E - 1) / Vec<T>::E, NW * 64};
+    float top;
+    int top_group;
+    const Sums mine = wave_join(stream(p, thread, top, top_group));
+    if (lane == 0) parts[wave] = mine;
+    if (out.top_k > 0) wave_top(p, thread, top, top_group, !(mine.s >= 0.f), out.top_k, lists + wave * out.top_k);
+    __syncthreads();
+    if (wave != 0) return;
+    Sums a = parts[0];
+#pragma unroll
+    for (int w = 1; w < NW; ++w) a = join(a, parts[w]);
+    const int64_t slot = at * splits + split;
+    if (lane == 0) {
+        if (splits == 1) put_row(row, classes, at, a, labels, out);
+        else sums[slot] = make_float4(a.m, a.s, a.t, 0.f);
+    }
+    if (out.top_k == 0) return;
+    if (splits == 1) {
+        const Row r = row_of(a);
+        merge_lists(lists, NW, out.top_k, lane, [&](int i, Key k) { put_top(out, at, i, k, r); });
+    } else {
+        merge_lists(lists, NW, out.top_k, lane, [&](int i, Key k) { keys[slot * out.top_k + i] = k; });
+    }
+}
+
+// One wavefront per row joins the parts (at most 64).
+template <typename T>
+__global__ __launch_bounds__(64) void logprob_join_k(const T *x, int64_t ld, int classes, int splits, const int64_t *labels,
+                                                     const LogprobOut out, const float4 *sums, const Key *keys) {
+    const int lane = (int)threadIdx.x;
+    const int64_t at = blockIdx.x;
+    Sums a{kLowest, 0.f, 0.f};
+    if (lane < splits) {
+        const float4 v = sums[at * splits + lane];
+        a = Sums{v.x, v.y, v.z};
+    }
+    a = wave_join(a);
+    if (lane == 0) put_row(x + at * ld, classes, at, a, labels, out);
+    if (out.top_k == 0) return;
+    const Row r = row_of(a);
+    merge_lists(keys + at * splits * out.top_k, splits, out.top_k, lane, [&](int i, Key k) { put_top(out, at, i, k, r); });
+}
+
+// ---- gradient ------------------------------------------------------------------------------------------------
+
+// 2^tshift neighbouring threads share a row; blockIdx.x counts pieces of kFly vectors a thread, blockIdx.y groups of rows.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t rows, int64_t ld, int classes, int tshift,
+                                                          const int64_t *labels, const float *lse, const float *entropy,
+                                                          const float *d_logprob, const float *d_entropy, float scale, T *out,
+                                                          int64_t out_ld) {
+    constexpr int E = Vec<T>::E;
+    const int team = 1 << tshift, per_block = kThreads >> tshift;
+    const int v0 = (int)blockIdx.x * team * kFly + ((int)threadIdx.x & (team - 1)), vecs = (classes + E - 1) / E;
+    for (int64_t at = (int64_t)blockIdx.y * per_block + ((int)threadIdx.x >> tshift); at < rows; at += (int64_t)gridDim.y * per_block) {
+        const T *row = x + at * ld;
+        T *to = out + at * out_ld;
+        const int64_t label = labels ? labels[at] : RVN_NO_LABEL;
+        const float norm = lse[at];
+        float given = 0.f, spread = 0.f, h = 0.f;
+        if (label != RVN_NO_LABEL) given = label >= 0 && label < classes ? scale * (d_logprob ? d_logprob[at] : 1.f) : __uint_as_float(0x7fc00000u);
+        if (d_entropy) spread = scale * d_entropy[at], h = entropy[at];
+        // a term whose weight is 0 is absent, whatever the row holds; so is every term of a row that has no class
+        const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            const int v = v0 + u * team;
+            if (v >= vecs) break;
+            float g[E];
+            if (none) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) g[e] = 0.f;
+            } else {
+                load_vec(row, v * E, classes, g);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float logp = g[e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
+                    float d = -given * p;
+                    if (d_entropy) d -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
+                    g[e] = label == v * E + e ? d + given : d;
+                }
+            }
+            if (v * E + E <= classes) {
+                *reinterpret_cast<u4_any *>(to + v * E) = Vec<T>::narrow(g);
+            } else {
+                for (int e = 0; v * E + e < classes; ++e) Vec<T>::put(to, v * E + e, g[e]);
+            }
+        }
+    }
+}
+
+struct Shape {
+    bool wave;           // a wavefront a row
+    int splits, share;   // else workgroups a row, and the classes of each
+};
+
+// Rows up to 8 KB go to one wavefront each; longer ones to a workgroup, or to several where there are fewer rows than
+// compute units and each still has 16 KB to read.
+Shape shape_of(int64_t rows, int classes, int size) {
+    const int64_t bytes = (int64_t)classes * size;
+    if (bytes <= 8192) return Shape{true, 1, classes};
+    if (rows >= 256) return Shape{false, 1, classes};
+    int64_t splits = (512 + rows - 1) / rows;
+    const int64_t most = (bytes + 16383) / 16384;
+    splits = splits < most ? splits : most;
+    splits = splits < 64 ? splits : 64;
+    const int step = 16 / size;
+    const int share = (int)(((classes + splits - 1) / splits + step - 1) / step * step);
+    return Shape{false, (classes + share - 1) / share, share};
+}
+
+template <typename T>
+void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch) {
+    const T *p = static_cast<const T *>(x.p);
+    const Shape s = shape_of(x.rows, x.classes, (int)sizeof(T));
+    const double bytes = (double)x.rows * ((double)x.classes * sizeof(T) + 20.0 + 12.0 * out.top_k);
+    if (!cx.launch(K_LOGPROB, bytes, 5.0 * (double)x.rows * x.classes)) return;
+    if (s.wave) {
+        const int per = kThreads / 64;
+        cx.run(logprob_wave_k<T>, dim3((unsigned)((x.rows + per - 1) / per)), dim3(kThreads), 0, p, x.rows, x.ld, x.classes, labels, out);
+        return;
+    }
+    float4 *sums = static_cast<float4 *>(scratch);
+    Key *keys = reinterpret_cast<Key *>(sums + (s.splits > 1 ? x.rows * s.splits : 0));
+    cx.run(logprob_block_k<T, 4>, dim3((unsigned)(x.rows * s.splits)), dim3(256), 0, p, x.ld, x.classes, s.splits, s.share, labels, out,
+           sums, keys);
+    if (s.splits == 1) return;
+    if (!cx.launch(K_LOGPROB, 0.0)) return;
+    cx.run(logprob_join_k<T>, dim3((unsigned)x.rows), dim3(64), 0, p, x.ld, x.classes, s.splits, labels, out, sums, keys);
+}
+
+template <typename T>
+void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,
+              const float *d_entropy, float scale, T *out, int64_t out_ld) {
+    if (!cx.launch(K_LOGPROB, (double)x.rows * (2.0 * x.classes * sizeof(T) + 16.0), 8.0 * (double)x.rows * x.classes)) return;
+    const int vecs = (x.classes + Vec<T>::E - 1) / Vec<T>::E;
+    int tshift = 0;
+    while (tshift < 8 && (kFly << tshift) < vecs) ++tshift;
+    const int64_t groups = (x.rows + (kThreads >> tshift) - 1) / (kThreads >> tshift);
+    const dim3 grid((unsigned)((vecs + (kFly << tshift) - 1) / (kFly << tshift)), (unsigned)(groups < 65535 ? groups : 65535));
+    cx.run(logprob_bwd_k<T>, grid, dim3(kThreads), 0, static_cast<const T *>(x.p), x.rows, x.ld, x.classes, tshift, labels, lse, entropy,
+           d_logprob, d_entropy, scale, out, out_ld);
+}
+
+}  // namespace
+
+size_t logprob_scratch_bytes(int64_t rows, int classes, int top_k) {
+    size_t most = 0;  // of the two types' shapes
+    for (int size = 2; size <= 4; size += 2) {
+        const Shape s = shape_of(rows, classes, size);
+        const size_t need = s.splits > 1 ? (size_t)rows * s.splits * (sizeof(float4) + (size_t)top_k * sizeof(Key)) : 0;
+        most = most > need ? most : need;
+    }
+    return most;
+}
+
+void logprob_fwd(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch) {
+    if (x.bf16) forward<Bf16>(cx, x, labels, out, scratch);
+    else forward<float>(cx, x, labels, out, scratch);
+}
+
+void logprob_bwd(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,
+                 const float *d_entropy, float scale, void *out, int64_t out_ld) {
+    if (x.bf16) backward(cx, x, labels, lse, entropy, d_logprob, d_entropy, scale, static_cast<Bf16 *>(out), out_ld);
+    else backward(cx, x, labels, lse, entropy, d_logprob, d_entropy, scale, static_cast<float *>(out), out_ld);
+}
+
+}  // namespace rvn

@@ -188,6 +188,37 @@ Plan make_plan(const rvn_block_desc &d, const Geo &g, bool backward, bool fixed)
 }
 
 
+StorePlan make_store_plan(const rvn_block_desc &d, const Geo &g) {
+    StorePlan s{};
+    Layer ly[3];
+    const int L = func_layers(d, ly);
+    size_t off = 0;
+    for (int l = 0; l < L; ++l) {
+        s.stats[l] = off;
+        off = align_up(off + kStatsArrays * (size_t)ly[l].cin * 4);
+        s.codes[l] = off;
+        s.scales[l] = off + ckpt_codes_bytes(ly[l].cin, g);
+        off = align_up(off + ckpt_bytes(ly[l].cin, g));
+    }
+    s.func = off;
+    return s;
+}
+
+StoredWs stored_bwd_ws(const Plan &p, const Geo &g) {
+    size_t sums = 0, widest = 0;
+    for (int l = 0; l < p.L; ++l) {
+        sums = std::max(sums, ckpt_bn_scratch_floats(p.layers[l].cin, g));
+        widest = std::max(widest, (size_t)p.layers[l].cin);
+    }
+    StoredWs w{p.total, p.h[0], align_up(p.total + sums * 4)};
+    const size_t need = (size_t)g.pixels() * widest * 4;
+    if (p.g[0] - p.h[0] < need) {
+        w.xf = w.total;
+        w.total = align_up(w.xf + need);
+    }
+    return w;
+}
+
 Bufs bind(const Plan &p, void *ws) {
     char *b = static_cast<char *>(ws);
     Bufs o{};
@@ -292,6 +323,18 @@ int check_ws(const void *ws, size_t have, size_t need) {
     return RVN_OK;
 }
 
+int check_store(const char *name, const void *p, size_t have, size_t need) {
+    if (!p) return fail(RVN_ERR_NULL, "%s is NULL (%zu bytes needed)", name, need);
+    if (reinterpret_cast<uintptr_t>(p) % kAlign) return fail(RVN_ERR_STRIDE, "%s is not %zu-byte aligned", name, kAlign);
+    if (have < need) return fail(RVN_ERR_SHAPE, "%s has %zu bytes, %zu needed", name, have, need);
+    return RVN_OK;
+}
+
+bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes) {
+    const uintptr_t pa = reinterpret_cast<uintptr_t>(a), pb = reinterpret_cast<uintptr_t>(b);
+    return pa < pb + b_bytes && pb < pa + a_bytes;
+}
+
 // ---- residual function drivers ----------------------------------------------
 
 // out = ep(r, Func(x)); leaves the layer inputs h_l and the BN statistics in `b`.
@@ -302,8 +345,10 @@ int check_ws(const void *ws, size_t have, size_t need) {
 // "Numerical error").
 // Returns where the statistics of layer 0 are: b.stats[0], or the spare array that a carried merge
 // filled ahead (see arm_merge); func_backward of the same function must be given that pointer.
+// keep != null: the checkpoint of every layer's input is left in keep[l] (floating-point stream, forward pass only).
 const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, const Bufs &b, Geo g, View x,
-                          const rvn_func_params &p, Epilogue ep, const View *r, View out, int frac_bits) {
+                          const rvn_func_params &p, Epilogue ep, const View *r, View out, int frac_bits,
+                          const Ckpt *keep = nullptr) {
     // the input's statistics may be there already
     const EmittedStats pm = cx.premerged;
     const float *const pm_stats = cx.premerged_stats;
@@ -344,6 +389,7 @@ const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
             cx.may_defer = false;
         }
         const float *scale_shift = (l == 0 ? stats0 : b.stats[l]) + 2 * ly.cin;
+        const View in = cur;
         if (l < pl.L - 1) {
             View h = dense_view(b.h[l], ly.cout, g);
             conv_fwd(cx, cur, scale_shift, d.conv_dtype, p.conv_w[l], wq, ly.cin, ly.cout, ly.ks, g, EP_STORE, nullptr, h, b.conv_scratch);
@@ -359,6 +405,8 @@ const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
         } else {
             conv_fwd(cx, cur, scale_shift, d.conv_dtype, p.conv_w[l], wq, ly.cin, ly.cout, ly.ks, g, ep, r, out, b.conv_scratch);
         }
+        // (after the convolution: a deferred merge leaves the statistics there only now)
+        if (keep) ckpt_save(cx, in, ly.cin, g, b.stats[l], keep[l]);
     }
     return stats0;
 }
@@ -469,6 +517,80 @@ void block_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, const Bufs 
     func_forward(cx, d, pl, b, g, y1, p.G, EP_ADD, &x2, y2, frac_bits);
 }
 
+// One function's place in a store: its statistics arrays take the place of the workspace's.
+struct StoredFunc {
+    Bufs b;
+    Ckpt k[3];
+};
+StoredFunc stored_func(const Plan &pl, const StorePlan &sp, const Bufs &b, char *at) {
+    StoredFunc f{b, {}};
+    for (int l = 0; l < pl.L; ++l) {
+        f.b.stats[l] = reinterpret_cast<float *>(at + sp.stats[l]);
+        f.k[l] = Ckpt{reinterpret_cast<int8_t *>(at + sp.codes[l]), reinterpret_cast<float *>(at + sp.scales[l])};
+    }
+    return f;
+}
+
+// func_backward with every layer's input read from its checkpoint: decoded for the two products of a layer, straight from
+// the codes for its BN backward pass.  sums, xf: see StoredWs.  Nothing has converted the function's filters: that
+// is the first launch.
+void func_backward_stored(Ctx &cx, const rvn_block_desc &d, const Plan &pl, const StoredFunc &f, Geo g, const rvn_func_params &p,
+                          View upstream, const rvn_func_grads &gr, bool accumulate, View skip, View out, float *sums, float *xf) {
+    const Bufs &b = f.b;
+    FilterPrep prep[3];
+    for (int l = 0; l < pl.L; ++l)
+        prep[l] = FilterPrep{p.conv_w[l], pl.layers[l].cin, pl.layers[l].cout, pl.layers[l].ks, nullptr, b.wq_b[l]};
+    double prep_bytes = 0.0;
+    const PrepArgs pa = plan_filter_prep(prep, pl.L, g, &prep_bytes);
+    if (pa.jobs > 0) prep_filters_bf16(cx, pa, prep_bytes);
+    View dh = upstream;
+    const uint16_t *dh16 = nullptr;
+    int cur = 0;
+    for (int l = pl.L - 1; l >= 0; --l) {
+        const Layer &ly = pl.layers[l];
+        const View xl = dense_view(xf, ly.cin, g);
+        ckpt_load(cx, f.k[l], ly.cin, g, xl);
+        WgradReduce red;
+        float *da = b.g[cur];
+        const float *const scale_shift = b.stats[l] + 2 * ly.cin;
+        const bool paired =
+            d.conv_dtype == RVN_F32
+                ? conv_dgrad_wgrad_f32(cx, xl, scale_shift, dh, p.conv_w[l], ly.cin, ly.cout, ly.ks, g, b.wgrad_scratch,
+                                       gr.d_conv_w[l], accumulate, da, &red)
+                : conv_dgrad_wgrad_bf16(cx, xl, scale_shift, dh, dh16, b.wq_b[l], ly.cin, ly.cout, ly.ks, g, b.wgrad_scratch,
+                                        gr.d_conv_w[l], accumulate, da, b.conv_scratch, &red);
+        if (!paired) {
+            if (dh16) {  // cannot happen: the layer above asked before it wrote bf16
+                cx.fail(hipErrorInvalidValue);
+                return;
+            }
+            conv_wgrad(cx, xl, scale_shift, d.conv_dtype, dh, ly.cin, ly.cout, ly.ks, g, b.wgrad_scratch, b.wgrad_floats,
+                       gr.d_conv_w[l], accumulate, &red);
+            conv_dgrad(cx, dh, d.conv_dtype, p.conv_w[l], b.wq_b[l], ly.cin, ly.cout, ly.ks, g, da, b.conv_scratch);
+        }
+        const View dav = dense_view(da, ly.cin, g);
+        if (l > 0) {
+            // (bf16 for the layer below where its shared launch takes it, as in func_backward)
+            const Layer &below = pl.layers[l - 1];
+            uint16_t *const as16 = reinterpret_cast<uint16_t *>(b.g[cur ^ 1]);
+            const bool to16 = d.conv_dtype == RVN_BF16 && g.hw() % 4 == 0 &&
+                              conv_dgrad_wgrad_takes_bf16_dh(dense_view(xf, below.cin, g), as16, b.wq_b[l - 1], below.cin, below.cout,
+                                                             below.ks, g, b.wgrad_scratch, da, b.conv_scratch);
+            ckpt_bn_relu_bwd(cx, f.k[l], dav, ly.cin, g, b.stats[l], sums, gr.d_bn_gamma[l], gr.d_bn_beta[l], accumulate, nullptr, dav,
+                             &red, to16 ? as16 : nullptr);
+            if (to16) {
+                dh16 = as16;
+            } else {
+                dh = dav;
+                dh16 = nullptr;
+                cur ^= 1;
+            }
+        } else {
+            ckpt_bn_relu_bwd(cx, f.k[0], dav, ly.cin, g, b.stats[0], sums, gr.d_bn_gamma[0], gr.d_bn_beta[0], accumulate, &skip, out, &red);
+        }
+    }
+}
+
 // Section 3.2, Algorithm 1, with G handled completely before F.  With a
 // fixed-point stream (frac_bits > 0) the tensors y, x hold int32 codes and the
 // derivatives stay fp32.
@@ -544,10 +666,37 @@ int check_bwd_args(const rvn_block_desc *desc, const rvn_tensor *y1, const rvn_t
 }
 
 void stack_forward(Ctx &cx, const rvn_block_desc &d, int depth, const Plan &pl, const Bufs &b, Geo g,
-                   View x1, View x2, const rvn_block_params *params, View y1, View y2, int frac_bits) {
+                   View x1, View x2, const rvn_block_params *params, View y1, View y2, int frac_bits, char *store) {
     clear_counters(cx, b.counters, pl.n_counters);
+    const StorePlan sp = store ? make_store_plan(d, g) : StorePlan{};
     for (int k = 0; k < depth; ++k) {
-        block_forward(cx, d, pl, b, g, k ? y1 : x1, k ? y2 : x2, params[k], y1, y2, frac_bits);
+        const View in1 = k ? y1 : x1, in2 = k ? y2 : x2;
+        if (!store) {
+            block_forward(cx, d, pl, b, g, in1, in2, params[k], y1, y2, frac_bits);
+            continue;
+        }
+        char *const at = store + sp.stack(k);
+        const StoredFunc F = stored_func(pl, sp, b, at), G = stored_func(pl, sp, b, at + sp.func);
+        func_forward(cx, d, pl, F.b, g, in2, params[k].F, EP_ADD, &in1, y1, 0, F.k);
+        func_forward(cx, d, pl, G.b, g, y1, params[k].G, EP_ADD, &in2, y2, 0, G.k);
+    }
+}
+
+// Ordinary backprop (Section 2.1) through the couplings, block by block from the top: dx1 = dy1 + (dG)^T dy2,
+// dx2 = dy2 + (dF)^T dx1.
+void stack_backward_stored(Ctx &cx, const rvn_block_desc &d, int depth, const Plan &pl, const Bufs &b, Geo g, View dy1, View dy2,
+                           const rvn_block_params *params, View dx1, View dx2, const rvn_block_grads *grads, bool accumulate,
+                           const char *store, void *ws) {
+    const StorePlan sp = make_store_plan(d, g);
+    const StoredWs at_ws = stored_bwd_ws(pl, g);
+    float *const sums = reinterpret_cast<float *>(static_cast<char *>(ws) + at_ws.sums);
+    float *const xf = reinterpret_cast<float *>(static_cast<char *>(ws) + at_ws.xf);
+    for (int k = depth - 1; k >= 0; --k) {
+        const View up1 = k == depth - 1 ? dy1 : dx1, up2 = k == depth - 1 ? dy2 : dx2;
+        char *const at = const_cast<char *>(store) + sp.stack(k);  // (read only: see func_backward_stored)
+        const StoredFunc F = stored_func(pl, sp, b, at), G = stored_func(pl, sp, b, at + sp.func);
+        func_backward_stored(cx, d, pl, G, g, params[k].G, up2, grads[k].G, accumulate, up1, dx1, sums, xf);
+        func_backward_stored(cx, d, pl, F, g, params[k].F, dx1, grads[k].F, accumulate, up2, dx2, sums, xf);
     }
 }
 
@@ -651,6 +800,78 @@ int revnet_stack_bwd(const rvn_block_desc *desc, int32_t depth, const rvn_tensor
     cx.stream = static_cast<hipStream_t>(hip_stream);
     stack_backward(cx, *desc, depth, pl, bind(pl, ws), g, view_of(y1), view_of(y2), view_of(dy1), view_of(dy2),
                    params, view_of(x1), view_of(x2), view_of(dx1), view_of(dx2), grads, accumulate_wgrads != 0);
+    return finish(cx);
+}
+
+int revnet_stack_stored_bytes(const rvn_block_desc *desc, int32_t depth, int64_t n, int64_t h, int64_t w, size_t *store_bytes,
+                              size_t *fwd_ws_bytes, size_t *bwd_ws_bytes) {
+    if (int rc = check_desc(desc)) return rc;
+    if (int rc = check_geo(n, h, w)) return rc;
+    if (depth <= 0) return fail(RVN_ERR_SHAPE, "depth = %d must be positive", depth);
+    const Geo g{(int)n, (int)h, (int)w};
+    if (store_bytes) *store_bytes = make_store_plan(*desc, g).stack(depth);
+    if (fwd_ws_bytes) *fwd_ws_bytes = make_plan(*desc, g, false).total;
+    if (bwd_ws_bytes) *bwd_ws_bytes = stored_bwd_ws(make_plan(*desc, g, true), g).total;
+    return RVN_OK;
+}
+
+int revnet_stack_fwd_stored(const rvn_block_desc *desc, int32_t depth, const rvn_tensor *x1, const rvn_tensor *x2,
+                            const rvn_block_params *params, const rvn_tensor *y1, const rvn_tensor *y2, void *store,
+                            size_t store_bytes, void *ws, size_t ws_bytes, void *hip_stream) {
+    Plan pl;
+    Geo g;
+    if (depth <= 0) return fail(RVN_ERR_SHAPE, "depth = %d must be positive", depth);
+    if (int rc = check_fwd_args(desc, x1, x2, y1, y2, ws, ws_bytes, &pl, &g, false)) return rc;
+    if (!params) return fail(RVN_ERR_NULL, "params is NULL");
+    for (int k = 0; k < depth; ++k)
+        if (int rc = check_params(*desc, &params[k], "params")) return rc;
+    const size_t need = make_store_plan(*desc, g).stack(depth);
+    if (int rc = check_store("store", store, store_bytes, need)) return rc;
+    if (ranges_overlap(store, need, ws, pl.total)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
+    const rvn_tensor *t[4] = {x1, x2, y1, y2};
+    for (const rvn_tensor *v : t)
+        if (overlaps_range(v, store, need)) return fail(RVN_ERR_ALIAS, "a tensor overlaps the store");
+    Ctx cx;
+    cx.stream = static_cast<hipStream_t>(hip_stream);
+    stack_forward(cx, *desc, depth, pl, bind(pl, ws), g, view_of(x1), view_of(x2), params, view_of(y1), view_of(y2), 0,
+                  static_cast<char *>(store));
+    return finish(cx);
+}
+
+int revnet_stack_bwd_stored(const rvn_block_desc *desc, int32_t depth, const rvn_tensor *dy1, const rvn_tensor *dy2,
+                            const rvn_block_params *params, const rvn_tensor *dx1, const rvn_tensor *dx2,
+                            const rvn_block_grads *grads, int accumulate_wgrads, const void *store, size_t store_bytes,
+                            void *ws, size_t ws_bytes, void *hip_stream) {
+    if (depth <= 0) return fail(RVN_ERR_SHAPE, "depth = %d must be positive", depth);
+    if (int rc = check_desc(desc)) return rc;
+    const rvn_tensor *t[4] = {dy1, dy2, dx1, dx2};
+    const char *nm[4] = {"dy1", "dy2", "dx1", "dx2"};
+    for (int i = 0; i < 4; ++i)
+        if (int rc = check_tensor(nm[i], t[i], *desc, i ? dy1 : nullptr)) return rc;
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j) {
+            if (j == i + 2 && same_tensor(t[i], t[j])) continue;  // dx_i in the place of dy_i
+            if (overlaps(t[i], t[j])) return fail(RVN_ERR_ALIAS, "%s and %s overlap", nm[i], nm[j]);
+        }
+    if (!params) return fail(RVN_ERR_NULL, "params is NULL");
+    if (!grads) return fail(RVN_ERR_NULL, "grads is NULL");
+    for (int k = 0; k < depth; ++k) {
+        if (int rc = check_params(*desc, &params[k], "params")) return rc;
+        if (int rc = check_grads(*desc, &grads[k], "grads")) return rc;
+    }
+    const Geo g{(int)dy1->n, (int)dy1->h, (int)dy1->w};
+    const Plan pl = make_plan(*desc, g, true);
+    const size_t ws_need = stored_bwd_ws(pl, g).total, need = make_store_plan(*desc, g).stack(depth);
+    if (int rc = check_ws(ws, ws_bytes, ws_need)) return rc;
+    if (int rc = check_store("store", store, store_bytes, need)) return rc;
+    if (ranges_overlap(store, need, ws, ws_need)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
+    for (int i = 0; i < 4; ++i)
+        if (overlaps_range(t[i], ws, ws_need) || overlaps_range(t[i], store, need))
+            return fail(RVN_ERR_ALIAS, "%s overlaps the workspace or the store", nm[i]);
+    Ctx cx;
+    cx.stream = static_cast<hipStream_t>(hip_stream);
+    stack_backward_stored(cx, *desc, depth, pl, bind(pl, ws), g, view_of(dy1), view_of(dy2), params, view_of(dx1), view_of(dx2), grads,
+                          accumulate_wgrads != 0, static_cast<const char *>(store), ws);
     return finish(cx);
 }
 

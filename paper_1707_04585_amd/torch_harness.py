@@ -38,15 +38,22 @@ class StackRunner:
     [N, C, H, W] buffer, i.e. strided views, unless split_buffers=True."""
 
     def __init__(self, kind, n, c, h, w, depth, width=None, conv="f32", eps=1e-5, device="cuda:0",
-                 split_buffers=False, frac_bits=0, **_unused):
+                 split_buffers=False, frac_bits=0, stored=False, **_unused):
         self.desc = B.BlockDesc(kind, c // 2, width or 0, eps, conv)
         self.n, self.c, self.h, self.w, self.depth = n, c, h, w, depth
         self.device = torch.device(device)
         self.split_buffers = split_buffers
         # frac_bits > 0: the residual stream is kept in fixed point (int32 codes of 2^-frac_bits)
         self.frac_bits = int(frac_bits)
-        query = B.revnet_fixed_workspace_bytes if self.frac_bits else B.revnet_workspace_bytes
-        self.fwd_bytes, self.bwd_bytes = query(self.desc, n, h, w)
+        # stored: every layer's input is kept in 8 bits and the backward pass recomputes nothing
+        self.store = None
+        assert not (stored and self.frac_bits)
+        if stored:
+            store_bytes, self.fwd_bytes, self.bwd_bytes = B.revnet_stack_stored_bytes(self.desc, depth, n, h, w)
+            self.store = torch.empty(store_bytes, dtype=torch.uint8, device=self.device)
+        else:
+            query = B.revnet_fixed_workspace_bytes if self.frac_bits else B.revnet_workspace_bytes
+            self.fwd_bytes, self.bwd_bytes = query(self.desc, n, h, w)
         self.ws = torch.empty(max(self.fwd_bytes, self.bwd_bytes), dtype=torch.uint8, device=self.device)
         self.params = self.grads = self._pp = self._pg = None
 
@@ -104,12 +111,19 @@ class StackRunner:
         if self.frac_bits:
             B.revnet_stack_fwd_fixed(self.desc, self.depth, self.frac_bits, xpair[1], xpair[2], self._pp, ypair[1],
                                      ypair[2], self.ws, stream)
+        elif self.store is not None:
+            B.revnet_stack_fwd_stored(self.desc, self.depth, xpair[1], xpair[2], self._pp, ypair[1], ypair[2], self.store,
+                                      self.ws, stream)
         else:
             B.revnet_stack_fwd(self.desc, self.depth, xpair[1], xpair[2], self._pp, ypair[1], ypair[2],
                                self.ws, stream)
 
     def backward(self, ypair, dypair, xpair, dxpair, accumulate=False, stream=None):
-        if self.frac_bits:
+        """(With a store ypair and xpair are not looked at: nothing is reconstructed.)"""
+        if self.store is not None:
+            B.revnet_stack_bwd_stored(self.desc, self.depth, dypair[1], dypair[2], self._pp, dxpair[1], dxpair[2], self._pg,
+                                      int(accumulate), self.store, self.ws, stream)
+        elif self.frac_bits:
             B.revnet_stack_bwd_fixed(self.desc, self.depth, self.frac_bits, ypair[1], ypair[2], dypair[1], dypair[2],
                                      self._pp, xpair[1], xpair[2], dxpair[1], dxpair[2], self._pg, int(accumulate),
                                      self.ws, stream)
@@ -120,9 +134,13 @@ class StackRunner:
 
     def activation_bytes(self):
         """Bytes alive between the end of forward and the end of backward:
-        top-of-stack activations, their gradients, and the backward workspace."""
+        top-of-stack activations, their gradients, the backward workspace and what is stored of the layers."""
         s = self.n * self.c * self.h * self.w * 4
-        return dict(stream=s, grads=s, workspace=self.bwd_bytes, total=2 * s + self.bwd_bytes)
+        out = dict(stream=s, grads=s, workspace=self.bwd_bytes, total=2 * s + self.bwd_bytes)
+        if self.store is not None:
+            out["store"] = self.store.numel()
+            out["total"] += out["store"]
+        return out
 
 
 def upload_down(P, device="cuda:0"):
@@ -146,7 +164,7 @@ class BodyRunner:
     and one gradient tensor per stage, whatever the stages' depths."""
 
     def __init__(self, kind, n, h, w, channels, depths, widths, conv="f32", eps=1e-5, device="cuda:0", frac_bits=0,
-                 **_unused):
+                 stored=False, **_unused):
         self.n, self.h, self.w, self.channels, self.depths = n, h, w, tuple(channels), tuple(depths)
         self.frac_bits = int(frac_bits)   # > 0: the stage tops hold fixed-point codes (int32 bit patterns in the fp32 tensors)
         self.device = torch.device(device)
@@ -154,8 +172,14 @@ class BodyRunner:
         downs = [B.DownDesc(kind, channels[s], channels[s + 1], 0, eps, conv) for s in range(len(channels) - 1)]
         self.down_descs = downs
         self.desc = B.BodyDesc(stages, depths, downs)
-        query = B.revnet_body_fixed_workspace_bytes if self.frac_bits else B.revnet_body_workspace_bytes
-        self.fwd_bytes, self.bwd_bytes = query(self.desc, n, h, w)
+        self.store = None   # stored: as in StackRunner
+        assert not (stored and self.frac_bits)
+        if stored:
+            store_bytes, self.fwd_bytes, self.bwd_bytes = B.revnet_body_stored_bytes(self.desc, n, h, w)
+            self.store = torch.empty(store_bytes, dtype=torch.uint8, device=self.device)
+        else:
+            query = B.revnet_body_fixed_workspace_bytes if self.frac_bits else B.revnet_body_workspace_bytes
+            self.fwd_bytes, self.bwd_bytes = query(self.desc, n, h, w)
         self.ws = torch.empty(max(self.fwd_bytes, self.bwd_bytes), dtype=torch.uint8, device=self.device)
         shape = lambda s: (n, channels[s], h >> s, w >> s)
         self.tops = [torch.empty(shape(s), dtype=torch.float32, device=self.device) for s in range(len(channels))]
@@ -174,6 +198,8 @@ class BodyRunner:
         """x: device tensor [n, channels[0], h, w]; it may be self.tops[0]."""
         if self.frac_bits:
             B.revnet_body_fwd_fixed(self.desc, self.frac_bits, x, self._sp, self._dp, self.tops, self.ws, stream)
+        elif self.store is not None:
+            B.revnet_body_fwd_stored(self.desc, x, self._sp, self._dp, self.tops, self.store, self.ws, stream)
         else:
             B.revnet_body_fwd(self.desc, x, self._sp, self._dp, self.tops, self.ws, stream)
 
@@ -182,6 +208,9 @@ class BodyRunner:
         if self.frac_bits:
             B.revnet_body_bwd_fixed(self.desc, self.frac_bits, self.tops, self.dtops, self._sp, self._dp, self._sg,
                                     self._dg, int(accumulate), self.ws, stream)
+        elif self.store is not None:
+            B.revnet_body_bwd_stored(self.desc, self.tops, self.dtops, self._sp, self._dp, self._sg, self._dg, int(accumulate),
+                                     self.store, self.ws, stream)
         else:
             B.revnet_body_bwd(self.desc, self.tops, self.dtops, self._sp, self._dp, self._sg, self._dg, int(accumulate),
                               self.ws, stream)
@@ -197,17 +226,59 @@ class BodyRunner:
     def activation_bytes(self):
         """Bytes alive between the end of forward and the end of backward."""
         acts = sum(t.numel() * 4 for t in self.tops)
-        return dict(stream=acts, grads=acts, workspace=self.bwd_bytes, total=2 * acts + self.bwd_bytes)
+        out = dict(stream=acts, grads=acts, workspace=self.bwd_bytes, total=2 * acts + self.bwd_bytes)
+        if self.store is not None:
+            out["store"] = self.store.numel()
+            out["total"] += out["store"]
+        return out
+
+
+class HeadRunner:
+    """Classification head on a top [n, c, h, w] and the scoring of its logits:
+    log probabilities of labels, entropy, the most likely classes, and the
+    gradient of the mean negative log likelihood."""
+
+    def __init__(self, head, n, h, w, top_k=5, eps=1e-5, device="cuda:0"):
+        classes, c = head["w"].shape
+        self.desc = B.HeadDesc(c, classes, eps)
+        self.device, self.n, self.classes, self.top_k = torch.device(device), n, classes, min(top_k, classes)
+        self.params = {k: _dev(head[k], self.device) for k in ("gamma", "beta", "w", "b")}
+        self.grads = {k: torch.zeros_like(v) for k, v in self.params.items()}
+        self._pp, self._pg = B.pack_head(self.params), B.pack_head(self.grads)
+        saved, bwd = B.revnet_head_workspace_bytes(self.desc, n, h, w)
+        empty = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=self.device)
+        self.saved = empty(saved, dtype=torch.uint8)
+        self.ws = empty(max(bwd, B.revnet_logprob_workspace_bytes(n, classes, self.top_k)), dtype=torch.uint8)
+        self.logits, self.d_logits = empty(n, classes), empty(n, classes)
+        self.logprob, self.entropy, self.lse = empty(n), empty(n), empty(n)
+        self.top_ids, self.top_logprob = empty(n, self.top_k, dtype=torch.int64), empty(n, self.top_k)
+
+    def forward(self, x, stream=None):
+        B.revnet_head_fwd(self.desc, x, self._pp, self.logits, self.saved, stream)
+
+    def score(self, labels, stream=None):
+        """labels: int64 [n]; fills logprob, entropy, lse, top_ids and top_logprob."""
+        B.revnet_logprob_fwd(self.logits, labels, self.top_k, self.logprob, self.entropy, self.lse, self.top_ids, self.top_logprob,
+                             self.ws, stream)
+
+    def backward(self, x, labels, dx, accumulate=False, stream=None):
+        """dx, self.grads: derivatives of -mean(logprob), after forward and score."""
+        B.revnet_logprob_bwd(self.logits, labels, self.lse, None, None, None, -1.0 / self.n, self.d_logits, stream)
+        B.revnet_head_bwd(self.desc, x, self.saved, self.d_logits, self._pp, dx, self._pg, int(accumulate), self.ws, stream)
 
 
 class NetRunner:
-    """Stem (image convolution, optional pooling) followed by a body: the whole
-    network up to the last stage's top.  Stored between forward and backward:
-    the image, the convolution's output when it is pooled, and one activation
-    per stage."""
+    """Stem (image convolution, optional pooling) followed by a body and, with
+    `head` (host arrays gamma, beta, w, b), a classification head.  Stored
+    between forward and backward: the image, the convolution's output when it
+    is pooled, one activation per stage, and what the body's store holds."""
 
-    def __init__(self, cfg, stem, device="cuda:0"):
+    def __init__(self, cfg, stem, device="cuda:0", head=None):
         self.body = BodyRunner(device=device, **cfg)
+        self.head = None
+        if head is not None:
+            top = self.body.tops[-1]
+            self.head = HeadRunner(head, *(top.shape[i] for i in (0, 2, 3)), device=device)
         self.device = self.body.device
         c0 = cfg["channels"][0]
         ks = int(stem["w"].shape[2])
@@ -222,7 +293,8 @@ class NetRunner:
     def set_params(self, stages, downs):
         self.body.set_params(stages, downs)
 
-    def forward(self, img, stream=None):
+    def forward(self, img, stream=None, labels=None):
+        """labels (int64 [n], with a head): the head's logits are scored as well."""
         n, _, h, w = img.shape
         if self.pool and self.conv_out is None:
             ho, wo = (h - 1) // self.stride + 1, (w - 1) // self.stride + 1
@@ -234,9 +306,16 @@ class NetRunner:
         # the stem writes the body's input into tops[0]; stage 0 then runs in place
         B.revnet_stem_fwd(self.stem_desc, img, self.stem_w, self.conv_out, self.body.tops[0], stream)
         self.body.forward(self.body.tops[0], stream)
+        if self.head is not None:
+            self.head.forward(self.body.tops[-1], stream)
+            if labels is not None:
+                self.head.score(labels, stream)
 
-    def backward(self, stream=None):
-        """body.dtops[-1] holds the upstream derivative."""
+    def backward(self, stream=None, labels=None):
+        """labels (with a head): derivatives of the mean negative log likelihood;
+        otherwise body.dtops[-1] holds the upstream derivative."""
+        if labels is not None:
+            self.head.backward(self.body.tops[-1], labels, self.body.dtops[-1], stream=stream)
         self.body.backward(stream=stream)
         B.revnet_stem_bwd(self.stem_desc, self.img, self.conv_out, self.body.dtops[0], self.stem_dw, 0, self.ws, stream)
 

@@ -1,0 +1,242 @@
+"""8-bit activation checkpoints on the GPU: the codes, scales and values bit for
+bit against the definition in numpy, and the backward pass of BN + ReLU from a
+checkpoint against the same formulas in 64 bits."""
+import numpy as np
+import pytest
+
+import operator_reference as R
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [  # n, c, h, w
+    (1, 1, 1, 1), (5, 3, 1, 1), (2, 5, 1, 3), (3, 7, 2, 2), (4, 8, 8, 8), (3, 5, 7, 7), (2, 3, 11, 12), (2, 4, 1, 127), (2, 4, 8, 16),
+    (2, 3, 3, 43), (9, 6, 16, 16), (3, 2, 27, 23), (2, 130, 14, 14), (1, 3, 60, 61),
+]
+
+
+def device(a):
+    import torch
+    return torch.as_tensor(np.ascontiguousarray(a)).cuda()
+
+
+def strided(a, layout):
+    """The array on the GPU: dense, as the second channel half of a wider tensor, with padded planes, or off 16-byte alignment."""
+    import torch
+    n, c, h, w = a.shape
+    t = torch.as_tensor(np.ascontiguousarray(a))
+    if layout == "dense":
+        return t.cuda()
+    if layout == "half":
+        full = torch.full((n, 2 * c, h, w), 7.0)
+        full[:, c:] = t
+        return full.cuda()[:, c:]
+    if layout == "padded":
+        full = torch.full((n, c, h + 1, w), 7.0)
+        full[:, :, :h] = t
+        return full.cuda()[:, :, :h]
+    flat = torch.full((a.size + 8,), 7.0).cuda()
+    view = flat[3:3 + a.size].view(n, c, h, w)
+    view.copy_(t)
+    return view
+
+
+def activations(rng, n, c, h, w):
+    return (rng.standard_normal((n, c, h, w)) * rng.uniform(0.5, 2, (c, 1, 1)) + rng.standard_normal((c, 1, 1))).astype(np.float32)
+
+
+def affine(rng, c):
+    return rng.uniform(0.5, 1.5, c) * np.where(rng.random(c) < 0.2, -1, 1), rng.standard_normal(c) * 0.1
+
+
+def unpack(buf, shape):
+    n, c, h, w = shape
+    host = buf.cpu().numpy()
+    codes = -(-n * c * h * w // 256) * 256
+    return host[:n * c * h * w].view(np.int8).reshape(shape), host[codes:].view(np.float32).reshape(n, c, -1)
+
+
+def pack(q, scales):
+    codes = -(-q.size // 256) * 256
+    buf = np.zeros(codes + scales.size * 4, np.uint8)
+    buf[:q.size] = q.reshape(-1).view(np.uint8)
+    buf[codes:] = scales.reshape(-1).view(np.uint8)
+    return device(buf)
+
+
+def save(x, stats, shape, fill=0xEE):
+    import torch
+    import paper_1707_04585_amd as rv
+    buf = torch.full((rv.revnet_ckpt_bytes(*shape),), fill, dtype=torch.uint8, device="cuda")
+    rv.revnet_ckpt_save(x, stats, buf)
+    return buf
+
+
+def same(a, b):
+    return np.array_equal(a.view(np.uint8) if a.dtype != np.float32 else a, b.view(np.uint8) if b.dtype != np.float32 else b, equal_nan=a.dtype == np.float32)
+
+
+@pytest.mark.parametrize("layout", ["dense", "half", "padded", "unaligned"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_save_and_load_are_the_definition(shape, layout):
+    import torch
+    import paper_1707_04585_amd as rv
+    rng = np.random.default_rng(sum(shape))
+    x = activations(rng, *shape)
+    x.flat[rng.integers(0, x.size, 1 + x.size // 50)] *= 40     # outliers
+    x[0, 0] = 0                                                 # a plane of zeros
+    stats = R.statistics(x, *affine(rng, shape[1])) if shape[0] * shape[2] * shape[3] > 1 else np.ones((4, shape[1]), np.float32)
+    for st in (None, stats):
+        q, s = R.encode(x, st)
+        buf = save(strided(x, layout), None if st is None else device(st), shape)
+        gq, gs = unpack(buf, shape)
+        assert same(gs, s) and np.array_equal(gq, q), (int((gq != q).sum()), x.size)
+        codes = -(-x.size // 256) * 256
+        assert (buf[x.size:codes] == 0xEE).all()                # nothing between codes and scales
+        out = strided(np.zeros(shape, np.float32), layout)
+        rv.revnet_ckpt_load(buf, out)
+        torch.cuda.synchronize()
+        got = out.cpu().numpy()
+        assert np.array_equal(got, R.decode(q, s))
+        if st is not None:
+            assert np.array_equal(R.positive(got, st), R.positive(x, st))
+        if layout == "half":
+            assert (out._base[:, :shape[1]] == 7).all()
+        if layout == "padded":
+            assert (out._base[:, :, shape[2]:] == 7).all()
+
+
+def test_extreme_values():
+    """Infinities, NaN, the largest and the smallest magnitudes, one group each."""
+    import torch
+    import paper_1707_04585_amd as rv
+    shape = (2, 4, 8, 64)   # four groups a plane
+    x = np.random.default_rng(5).standard_normal(shape).astype(np.float32)
+    flat = x.reshape(2, 4, 4, 128)
+    flat[0, 0, 0, 5] = np.inf
+    flat[0, 0, 1, 127] = np.nan
+    flat[0, 1, 0, 0] = -np.inf
+    flat[0, 1, 1] = np.float32(3.4e38) * np.where(np.arange(128) % 2, 1, -1)
+    flat[0, 2, 0] = 0
+    flat[0, 2, 1] = np.float32(1e-45)
+    flat[0, 2, 2] *= np.float32(1e-41)
+    flat[0, 3, 0] *= np.float32(1e-37)
+    flat[1, 0, 0] = -0.0
+    q, s = R.encode(x)
+    buf = save(device(x), None, shape)
+    gq, gs = unpack(buf, shape)
+    assert same(gs, s) and np.array_equal(gq, q)
+    y = torch.zeros(shape, device="cuda")
+    rv.revnet_ckpt_load(buf, y)
+    got = y.cpu().numpy().reshape(flat.shape)
+    for at in ((0, 0, 0), (0, 0, 1), (0, 1, 0)):
+        assert np.isnan(got[at]).all()
+    assert np.isfinite(got[0, 0, 2]).all() and np.isfinite(got[0, 1, 1]).all() and (got[0, 2, :2] == 0).all()
+
+
+def run_bwd(buf, stats, da, skip, dx, c, shape, accumulate=0, start=0.0, stream=None):
+    import torch
+    import paper_1707_04585_amd as rv
+    dg, db = torch.full((c,), start, device="cuda"), torch.full((c,), 2 * start, device="cuda")
+    ws = torch.full((max(256, rv.revnet_ckpt_bn_relu_workspace_bytes(*shape)),), 0xFF, dtype=torch.uint8, device="cuda")
+    rv.revnet_ckpt_bn_relu_bwd(buf, stats, da, skip, dx, dg, db, accumulate, ws, stream)
+    return dg, db
+
+
+BWD_SHAPES = [s for s in SHAPES if s[0] * s[2] * s[3] >= 4] + [
+    (40, 16, 32, 32),     # two launches, many workgroups a channel
+    (33, 300, 9, 11),     # one launch, 256 threads
+    (30, 280, 28, 28),    # one launch, 1024 threads
+    (6, 2100, 45, 45),    # two launches, one workgroup's sums a channel
+    (300, 3, 1, 5),
+]
+
+
+@pytest.mark.parametrize("shape,layout", [(s, l) for s in BWD_SHAPES for l in ("dense", "half", "unaligned") if l == "dense" or np.prod(s) <= 4e6])
+def test_backward_pass_of_bn_relu_from_codes(shape, layout):
+    import torch
+    n, c, h, w = shape
+    rng = np.random.default_rng(n * c + h * w)
+    x = activations(rng, *shape)
+    stats = R.statistics(x, *affine(rng, c))
+    q, s = R.encode(x, stats)
+    da, skip = rng.standard_normal(shape).astype(np.float32), rng.standard_normal(shape).astype(np.float32)
+    buf, st = pack(q, s), device(stats)
+    for sk in (None, skip):
+        dx, dg, db, tol = R.bn_relu_bwd(R.decode(q, s), stats, da, sk)
+        out = strided(np.zeros(shape, np.float32), layout)
+        gd, gb = run_bwd(buf, st, strided(da, layout), None if sk is None else strided(sk, layout), out, c, shape)
+        torch.cuda.synchronize()
+        for name, got, ref, t in (("dx", out, dx, tol["dx"]), ("d_gamma", gd, dg, tol["dg"]), ("d_beta", gb, db, tol["db"])):
+            off = np.abs(got.cpu().numpy().astype(np.float64) - ref)
+            assert np.all(off <= t), (name, float((off / np.maximum(t, 1e-300)).max()))
+        if layout == "half":
+            assert (out._base[:, :c] == 7).all()
+
+
+def test_backward_in_place_accumulating_and_again():
+    """dx over da and over skip, gradients added to, the same bits from the same call."""
+    import torch
+    for shape in ((5, 6, 9, 9), (40, 16, 32, 32)):
+        rng = np.random.default_rng(9)
+        c = shape[1]
+        x = activations(rng, *shape)
+        stats = R.statistics(x, *affine(rng, c))
+        buf, st = pack(*R.encode(x, stats)), device(stats)
+        da, skip = device(rng.standard_normal(shape).astype(np.float32)), device(rng.standard_normal(shape).astype(np.float32))
+        plain, with_skip = torch.empty_like(da), torch.empty_like(da)
+        dg, db = run_bwd(buf, st, da, None, plain, c, shape)
+        run_bwd(buf, st, da, skip, with_skip, c, shape)
+        again = torch.empty_like(da)
+        dg2, db2 = run_bwd(buf, st, da, None, again, c, shape)
+        assert torch.equal(plain, again) and torch.equal(dg, dg2) and torch.equal(db, db2)
+        over_da, over_skip = da.clone(), skip.clone()
+        ag, ab = run_bwd(buf, st, over_da, None, over_da, c, shape, accumulate=1, start=1.5)
+        run_bwd(buf, st, da, over_skip, over_skip, c, shape)
+        assert torch.equal(over_da, plain) and torch.equal(over_skip, with_skip)
+        assert torch.equal(ag, dg + 1.5) and torch.equal(ab, db + 3.0)
+
+
+def test_on_another_stream_and_in_a_graph():
+    """Save, load and backward captured into one graph: every replay gives the eager calls' bits, also after the inputs
+    have changed and with eager calls in between."""
+    import torch
+    import paper_1707_04585_amd as rv
+    shape = (40, 16, 32, 32)
+    rng = np.random.default_rng(3)
+    c = shape[1]
+    x = device(activations(rng, *shape))
+    stats = device(R.statistics(x.cpu().numpy(), *affine(rng, c)))
+    da = device(rng.standard_normal(shape).astype(np.float32))
+
+    def buffers():
+        return dict(buf=torch.empty(rv.revnet_ckpt_bytes(*shape), dtype=torch.uint8, device="cuda"), y=torch.empty_like(x), dx=torch.empty_like(x),
+                    dg=torch.empty(c, device="cuda"), db=torch.empty(c, device="cuda"),
+                    ws=torch.empty(rv.revnet_ckpt_bn_relu_workspace_bytes(*shape), dtype=torch.uint8, device="cuda"))
+
+    def step(b, stream):
+        rv.revnet_ckpt_save(x, stats, b["buf"], stream)
+        rv.revnet_ckpt_load(b["buf"], b["y"], stream)
+        rv.revnet_ckpt_bn_relu_bwd(b["buf"], stats, da, None, b["dx"], b["dg"], b["db"], 0, b["ws"], stream)
+
+    own, eager = buffers(), buffers()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    step(own, side)          # on a stream of its own
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(own, torch.cuda.current_stream())
+    for k in range(4):
+        x.mul_(1.0 + 0.25 * k)
+        da.mul_(-1.5)
+        for t in own.values():
+            t.zero_()
+        graph.replay()
+        step(eager, torch.cuda.current_stream())
+        torch.cuda.synchronize()
+        for name in ("buf", "y", "dx", "dg", "db"):
+            if name == "buf":
+                a, b = unpack(own[name], shape), unpack(eager[name], shape)
+                assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+            else:
+                assert torch.equal(own[name], eager[name]), name
