@@ -9,10 +9,12 @@
 // The sums are fp32: at most a few hundred terms in a thread, then a tree.
 //
 // Top classes.  Classes are ordered by one 64-bit key: the value's bits made monotonic, above the complement of the class
-// number, so that no two are equal.  A thread knows the largest key of its own vectors; a wavefront takes the largest
-// among its threads, and only the one thread that gave it looks for its next smaller key, for which the whole wavefront
-// reads that thread's vectors (at most one vector a lane for rows up to 64 * 64 vectors per wavefront).  Each wavefront lists
-// its first top_k this way, and the lists are merged.
+// number, so that no two are equal.  Every thread of a row knows the largest value of its own vectors; the top_k-th largest
+// of these (to 16 bits, by bisection: count the threads at or above a bit pattern) bounds the top_k-th largest class from
+// below.  The few classes at or above the bound are listed -- a thread reads again only the group of vectors that holds its
+// largest, or all of its own where a second group reaches the bound -- and each takes the place that the number of larger keys
+// in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
+// wavefront takes its largest keys one by one and the lists are merged.
 #include "kernels.h"
 
 namespace rvn {
@@ -72,16 +74,25 @@ struct Vec<Bf16> {
     }
 };
 
-// The vector that starts at class `at` of a row of `classes` > at; what lies behind the row reads as -infinity.
+// The vector that starts at class `at` (which may be up to E - 1 before the row's first) of a row of `classes`; what lies
+// outside the row reads as -infinity.
 template <typename T>
 __device__ __forceinline__ void load_vec(const T *row, int at, int classes, float (&v)[Vec<T>::E]) {
     constexpr int E = Vec<T>::E;
-    if (at + E <= classes) {
+    if (at >= 0 && at + E <= classes) {
         Vec<T>::widen(*reinterpret_cast<const u4_any *>(row + at), v);
     } else {
 #pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = at + e < classes ? Vec<T>::one(row, at + e) : -INFINITY;
+        for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < classes ? Vec<T>::one(row, at + e) : -INFINITY;
     }
+}
+
+// Elements from the last 16-byte border to p: the vectors of a row start that much before it, so that their accesses are
+// aligned wherever the row begins.  (Rows of an odd number of bf16 logits, 4096 x 50021: 98.6 us with vectors from the row's
+// start, 77.5 where the rows are aligned by themselves.)
+template <typename T>
+__device__ __forceinline__ int skew_of(const T *p) {
+    return (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
 }
 
 // Bits that order as the values do, -0 as 0, NaN above all; never 0, and never 0xffffffff, which is above every key.
@@ -133,25 +144,17 @@ __device__ __forceinline__ Sums wave_join(Sums v) {
     return v;
 }
 
-// A team of NT threads on classes [first, last) of a row: vector v of that part belongs to thread v % NT.
+// A team of NT threads on `length` classes of a row from class `first`: vector v of that part, its classes
+// v * E - skew .. + E - 1, belongs to thread v % NT.
 template <typename T>
 struct Part {
     const T *row;  // at class `first`
-    int first, length, vecs, NT;
-};
-
-template <typename T>
-__device__ __forceinline__ Key best_below(const Part<T> &p, int v, Key below, Key best) {
-    constexpr int E = Vec<T>::E;
-    float x[E];
-    load_vec(p.row, v * E, p.length, x);
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const Key k{order_bits(x[e]), 0xffffffffu - (uint32_t)(p.first + v * E + e)};
-        if (v * E + e < p.length && less(k, below) && less(best, k)) best = k;
+    int first, length, skew, vecs, NT;
+    __device__ __forceinline__ Part(const T *r, int f, int l, int nt) : row(r), first(f), length(l), skew(skew_of(r)), NT(nt) {
+        vecs = (l + skew + Vec<T>::E - 1) / Vec<T>::E;
     }
-    return best;
-}
+    __device__ __forceinline__ int at(int v) const { return v * Vec<T>::E - skew; }
+};
 
 template <typename T>
 __device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T>::E], float most) {
@@ -171,24 +174,28 @@ __device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T
         }
 }
 
-// The sums of a thread's vectors, and where its largest value is: the first group of kFly vectors that holds it.
+// The largest value of a thread's vectors, the first group of kFly vectors that holds it, and the largest of the others.
+struct Top {
+    float value, second;
+    int group;
+};
+
 template <typename T>
-__device__ __forceinline__ Sums stream(const Part<T> &p, int thread, float &top, int &top_group) {
+__device__ __forceinline__ Sums stream(const Part<T> &p, int thread, Top &top) {
     constexpr int E = Vec<T>::E;
     Sums a{kLowest, 0.f, 0.f};
-    top = -INFINITY;
-    top_group = 0;
+    top = Top{-INFINITY, -INFINITY, 0};
     for (int g = 0; thread + g * kFly * p.NT < p.vecs; ++g) {
         float x[kFly][E];
         const int v0 = thread + g * kFly * p.NT;
-        if ((v0 + (kFly - 1) * p.NT) * E + E <= p.length) {
+        if (p.at(v0) >= 0 && p.at(v0 + (kFly - 1) * p.NT) + E <= p.length) {
 #pragma unroll
-            for (int u = 0; u < kFly; ++u) Vec<T>::widen(*reinterpret_cast<const u4_any *>(p.row + (v0 + u * p.NT) * E), x[u]);
+            for (int u = 0; u < kFly; ++u) Vec<T>::widen(*reinterpret_cast<const u4_any *>(p.row + p.at(v0 + u * p.NT)), x[u]);
         } else {
 #pragma unroll
             for (int u = 0; u < kFly; ++u) {
                 if (v0 + u * p.NT < p.vecs) {
-                    load_vec(p.row, (v0 + u * p.NT) * E, p.length, x[u]);
+                    load_vec(p.row, p.at(v0 + u * p.NT), p.length, x[u]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[u][e] = -INFINITY;
@@ -200,28 +207,120 @@ __device__ __forceinline__ Sums stream(const Part<T> &p, int thread, float &top,
         for (int u = 0; u < kFly; ++u)
 #pragma unroll
             for (int e = 0; e < E; ++e) most = fmaxf(most, x[u][e]);
-        if (most > top) {
-            top = most;
-            top_group = g;
-        }
+        const bool up = most > top.value;
+        top.second = fmaxf(top.second, up ? top.value : most);
+        if (up) top.value = most, top.group = g;
         add_values<T>(a, x, most);
     }
     return a;
 }
 
-// list[0 .. top_k) = the largest keys of the vectors of one wavefront's threads in falling order, then {0, 0}.  Every
-// lane of the wavefront is active.  nan: the part holds one (no thread's `top` counts it).
+// ---- the top classes of a part, by a bound -------------------------------------------------------------------------
+
+constexpr int kListed = 256;  // keys that a team's list holds
+
+template <int NW>
+struct TeamLds {
+    Key list[kListed];
+    uint32_t tops[NW * 64];
+    int listed;
+};
+
+template <int NW>
+__device__ __forceinline__ void team_barrier() {
+    if constexpr (NW == 1) __builtin_amdgcn_wave_barrier();
+    else __syncthreads();
+}
+
+// Lists the classes of vector v whose order bits reach `bound`.
 template <typename T>
-__device__ __forceinline__ void wave_top(const Part<T> &p, int thread, float top, int top_group, bool nan, int top_k, Key *list) {
+__device__ __forceinline__ void list_vector(const Part<T> &p, int v, uint32_t bound, Key *list, int *listed) {
+    constexpr int E = Vec<T>::E;
+    float x[E];
+    load_vec(p.row, p.at(v), p.length, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const uint32_t order = order_bits(x[e]);
+        const int i = p.at(v) + e;
+        if (order >= bound && i >= 0 && i < p.length) {
+            const int slot = atomicAdd(listed, 1);
+            if (slot < kListed) list[slot] = Key{order, 0xffffffffu - (uint32_t)(p.first + i)};
+        }
+    }
+}
+
+// Fills lds.list with lds.listed keys among which are the part's top_k largest (or all that it has).  More than kListed:
+// the list is not complete.  The part holds no NaN.  All threads of the team call it; the last barrier is the caller's.
+template <typename T, int NW>
+__device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top &top, int top_k, TeamLds<NW> &lds) {
+    const bool has = thread < p.vecs;
+    const uint32_t mine = has ? order_bits(top.value) : 0u;
+    uint32_t seen[NW];
+    if (thread == 0) lds.listed = 0;
+    if constexpr (NW == 1) {
+        seen[0] = mine;
+    } else {
+        lds.tops[thread] = mine;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < NW; ++w) seen[w] = lds.tops[w * 64 + (thread & 63)];
+    }
+    team_barrier<NW>();
+    uint32_t bound = 0;
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t next = bound | 1u << bit;
+        int count = 0;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) count += __popcll(__ballot(seen[w] >= next));
+        if (count >= top_k) bound = next;
+    }
+    if (has && mine >= bound) {
+        const bool all = order_bits(top.second) >= bound;
+        const int g0 = all ? 0 : top.group, g1 = all ? (p.vecs + kFly * p.NT - 1) / (kFly * p.NT) : top.group + 1;
+        for (int g = g0; g < g1; ++g)
+#pragma unroll
+            for (int u = 0; u < kFly; ++u) {
+                const int v = thread + (g * kFly + u) * p.NT;
+                if (v < p.vecs) list_vector(p, v, bound, lds.list, &lds.listed);
+            }
+    }
+}
+
+// place(r, key) for the top_k largest of `count` <= kListed keys, each by one thread: r keys are larger.
+template <typename Place>
+__device__ __forceinline__ void place_top(const Key *list, int count, int top_k, int thread, int threads, Place place) {
+    for (int i = thread; i < count; i += threads) {
+        const Key k = list[i];
+        int larger = 0;
+        for (int j = 0; j < count; ++j) larger += less(k, list[j]) ? 1 : 0;
+        if (larger < top_k) place(larger, k);
+    }
+}
+
+// ---- the same one by one: ties beyond the list, NaN ----------------------------------------------------------------
+
+template <typename T>
+__device__ __forceinline__ Key best_below(const Part<T> &p, int v, Key below, Key best) {
+    constexpr int E = Vec<T>::E;
+    float x[E];
+    load_vec(p.row, p.at(v), p.length, x);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+        const int i = p.at(v) + e;
+        const Key k{order_bits(x[e]), 0xffffffffu - (uint32_t)(p.first + i)};
+        if (i >= 0 && i < p.length && less(k, below) && less(best, k)) best = k;
+    }
+    return best;
+}
+
+// list[0 .. top_k) = the largest keys of the vectors of one wavefront's threads in falling order, then {0, 0}.  Every
+// lane of the wavefront is active.
+template <typename T>
+__device__ __forceinline__ void wave_top(const Part<T> &p, int thread, int top_k, Key *list) {
     const int lane = thread & 63;
     const Key above{0xffffffffu, 0xffffffffu};
     Key mine{0u, 0u};
-    const int g0 = nan ? 0 : top_group, g1 = nan ? (p.vecs + kFly * p.NT - 1) / (kFly * p.NT) : top_group + 1;
-    for (int g = g0; g < g1; ++g)
-        for (int u = 0; u < kFly; ++u) {
-            const int v = thread + (g * kFly + u) * p.NT;
-            if (v < p.vecs) mine = best_below(p, v, above, mine);
-        }
+    for (int v = thread; v < p.vecs; v += p.NT) mine = best_below(p, v, above, mine);
     for (int r = 0; r < top_k; ++r) {
         const Key most = wave_most(mine);
         if (lane == 0) list[r] = most;
@@ -230,6 +329,7 @@ __device__ __forceinline__ void wave_top(const Part<T> &p, int thread, float top
             return;
         }
         if (r + 1 == top_k) return;
+        // the one thread that gave it looks for its next: the wavefront reads that thread's vectors
         const int winner = __ffsll((unsigned long long)__ballot(mine.hi == most.hi && mine.lo == most.lo)) - 1;
         Key next{0u, 0u};
         for (int v = (thread - lane) + winner + lane * p.NT; v < p.vecs; v += 64 * p.NT) next = best_below(p, v, most, next);
@@ -251,6 +351,27 @@ __device__ __forceinline__ void merge_lists(const Key *keys, int lists, int top_
             mine = at < top_k ? keys[lane * top_k + at] : Key{0u, 0u};
         }
     }
+}
+
+// place(r, key) for the r-th largest class of the part, r < top_k ({0, 0} where the part has fewer).  nan: the part holds
+// one.  All threads of the team call it, with the same nan.
+template <typename T, int NW, typename Place>
+__device__ __forceinline__ void team_top(const Part<T> &p, int thread, const Top &top, bool nan, int top_k, TeamLds<NW> &lds, Place place) {
+    if (!nan) {
+        list_top(p, thread, top, top_k, lds);
+        team_barrier<NW>();
+        const int count = lds.listed;
+        if (count <= kListed) {
+            for (int r = count + thread; r < top_k; r += NW * 64) place(r, Key{0u, 0u});
+            place_top(lds.list, count, top_k, thread, NW * 64, place);
+            return;
+        }
+        team_barrier<NW>();  // (every thread has read the count)
+    }
+    static_assert(NW * RVN_MAX_TOP_K <= kListed, "a list for every wavefront");
+    wave_top(p, thread, top_k, lds.list + (thread >> 6) * top_k);
+    team_barrier<NW>();
+    if (thread < 64) merge_lists(lds.list, NW, top_k, thread, place);
 }
 
 // One lane writes a row's results.
@@ -287,20 +408,17 @@ __device__ __forceinline__ void put_top(const LogprobOut &out, int64_t at, int r
 template <typename T>
 __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t rows, int64_t ld, int classes, const int64_t *labels,
                                                            const LogprobOut out) {
-    __shared__ Key lists[kThreads / 64][RVN_MAX_TOP_K];
+    __shared__ TeamLds<1> lds[kThreads / 64];
     const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
     const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + wave;
     if (at >= rows) return;
-    const Part<T> p{x + at * ld, 0, classes, (classes + Vec<T>::E - 1) / Vec<T>::E, 64};
-    float top;
-    int top_group;
-    const Sums a = wave_join(stream(p, lane, top, top_group));
+    const Part<T> p(x + at * ld, 0, classes, 64);
+    Top top;
+    const Sums a = wave_join(stream(p, lane, top));
     if (lane == 0) put_row(p.row, classes, at, a, labels, out);
     if (out.top_k == 0) return;
-    wave_top(p, lane, top, top_group, !(a.s >= 0.f), out.top_k, lists[wave]);
-    __builtin_amdgcn_wave_barrier();
     const Row row = row_of(a);
-    if (lane < out.top_k) put_top(out, at, lane, lists[wave][lane], row);
+    team_top<T, 1>(p, lane, top, row.nan, out.top_k, lds[wave], [&](int i, Key k) { put_top(out, at, i, k, row); });
 }
 
 // A workgroup of NW wavefronts per part of a row.  splits == 1: the whole row, results written here.  Otherwise the
@@ -308,54 +426,66 @@ __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t r
 template <typename T, int NW>
 __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t ld, int classes, int splits, int share,
                                                            const int64_t *labels, const LogprobOut out, float4 *sums, Key *keys) {
-    __shared__ Key lists[NW * RVN_MAX_TOP_K];
+    __shared__ TeamLds<NW> lds;
     __shared__ Sums parts[NW];
     const int thread = (int)threadIdx.x, wave = thread >> 6, lane = thread & 63;
     const int64_t at = splits == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)splits);
     const int split = splits == 1 ? 0 : (int)(blockIdx.x - (unsigned)at * (unsigned)splits);
-    const int first = split * share, length = min(share, classes - first);
+    const int first = split * share;
     const T *row = x + at * ld;
-    const Part<T> p{row + first, first, length, (length + Vec<T>::E - 1) / Vec<T>::E, NW * 64};
-    float top;
-    int top_group;
-    const Sums mine = wave_join(stream(p, thread, top, top_group));
+    const Part<T> p(row + first, first, min(share, classes - first), NW * 64);
+    Top top;
+    const Sums mine = wave_join(stream(p, thread, top));
     if (lane == 0) parts[wave] = mine;
-    if (out.top_k > 0) wave_top(p, thread, top, top_group, !(mine.s >= 0.f), out.top_k, lists + wave * out.top_k);
     __syncthreads();
-    if (wave != 0) return;
     Sums a = parts[0];
 #pragma unroll
     for (int w = 1; w < NW; ++w) a = join(a, parts[w]);
     const int64_t slot = at * splits + split;
-    if (lane == 0) {
+    if (thread == 0) {
         if (splits == 1) put_row(row, classes, at, a, labels, out);
         else sums[slot] = make_float4(a.m, a.s, a.t, 0.f);
     }
     if (out.top_k == 0) return;
-    if (splits == 1) {
-        const Row r = row_of(a);
-        merge_lists(lists, NW, out.top_k, lane, [&](int i, Key k) { put_top(out, at, i, k, r); });
-    } else {
-        merge_lists(lists, NW, out.top_k, lane, [&](int i, Key k) { keys[slot * out.top_k + i] = k; });
-    }
+    const Row r = row_of(a);
+    team_top<T, NW>(p, thread, top, r.nan, out.top_k, lds, [&](int i, Key k) {
+        if (splits == 1) put_top(out, at, i, k, r);
+        else keys[slot * out.top_k + i] = k;
+    });
 }
 
-// One wavefront per row joins the parts (at most 64).
+// Joins the parts (at most 64) of a row.  A part's last key bounds the row's top_k-th from below; what reaches the largest
+// of these bounds is listed and placed as above.
 template <typename T>
-__global__ __launch_bounds__(64) void logprob_join_k(const T *x, int64_t ld, int classes, int splits, const int64_t *labels,
-                                                     const LogprobOut out, const float4 *sums, const Key *keys) {
-    const int lane = (int)threadIdx.x;
+__global__ __launch_bounds__(kThreads) void logprob_join_k(const T *x, int64_t ld, int classes, int splits, const int64_t *labels,
+                                                           const LogprobOut out, const float4 *sums, const Key *keys) {
+    __shared__ Key list[kListed];
+    __shared__ int listed;
+    const int thread = (int)threadIdx.x, lane = thread & 63, top_k = out.top_k;
     const int64_t at = blockIdx.x;
+    const Key *row_keys = keys + at * splits * top_k;
     Sums a{kLowest, 0.f, 0.f};
+    Key last{0u, 0u};
     if (lane < splits) {
         const float4 v = sums[at * splits + lane];
         a = Sums{v.x, v.y, v.z};
+        if (top_k > 0) last = row_keys[lane * top_k + top_k - 1];
     }
     a = wave_join(a);
-    if (lane == 0) put_row(x + at * ld, classes, at, a, labels, out);
-    if (out.top_k == 0) return;
+    if (thread == 0) put_row(x + at * ld, classes, at, a, labels, out), listed = 0;
+    if (top_k == 0) return;
     const Row r = row_of(a);
-    merge_lists(keys + at * splits * out.top_k, splits, out.top_k, lane, [&](int i, Key k) { put_top(out, at, i, k, r); });
+    const Key bound = wave_most(last);
+    __syncthreads();
+    for (int i = thread; i < splits * top_k; i += kThreads) {
+        const Key k = row_keys[i];
+        if (k.hi == 0u || less(k, bound)) continue;
+        const int slot = atomicAdd(&listed, 1);
+        if (slot < kListed) list[slot] = k;
+    }
+    __syncthreads();
+    if (listed <= kListed) place_top(list, listed, top_k, thread, kThreads, [&](int i, Key k) { put_top(out, at, i, k, r); });
+    else if (thread < 64) merge_lists(row_keys, splits, top_k, lane, [&](int i, Key k) { put_top(out, at, i, k, r); });
 }
 
 // ---- gradient ------------------------------------------------------------------------------------------------
@@ -368,10 +498,11 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
                                                           int64_t out_ld) {
     constexpr int E = Vec<T>::E;
     const int team = 1 << tshift, per_block = kThreads >> tshift;
-    const int v0 = (int)blockIdx.x * team * kFly + ((int)threadIdx.x & (team - 1)), vecs = (classes + E - 1) / E;
+    const int v0 = (int)blockIdx.x * team * kFly + ((int)threadIdx.x & (team - 1));
     for (int64_t at = (int64_t)blockIdx.y * per_block + ((int)threadIdx.x >> tshift); at < rows; at += (int64_t)gridDim.y * per_block) {
         const T *row = x + at * ld;
         T *to = out + at * out_ld;
+        const int skew = skew_of(to), vecs = (classes + skew + E - 1) / E;
         const int64_t label = labels ? labels[at] : RVN_NO_LABEL;
         const float norm = lse[at];
         float given = 0.f, spread = 0.f, h = 0.f;
@@ -381,26 +512,28 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
         const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
-            const int v = v0 + u * team;
+            const int v = v0 + u * team, first = v * E - skew;
             if (v >= vecs) break;
             float g[E];
             if (none) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) g[e] = 0.f;
             } else {
-                load_vec(row, v * E, classes, g);
+                load_vec(row, first, classes, g);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     const float logp = g[e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
                     float d = -given * p;
                     if (d_entropy) d -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
-                    g[e] = label == v * E + e ? d + given : d;
+                    g[e] = label == first + e ? d + given : d;
                 }
             }
-            if (v * E + E <= classes) {
-                *reinterpret_cast<u4_any *>(to + v * E) = Vec<T>::narrow(g);
+            if (first >= 0 && first + E <= classes) {
+                *reinterpret_cast<u4 *>(to + first) = Vec<T>::narrow(g);
             } else {
-                for (int e = 0; v * E + e < classes; ++e) Vec<T>::put(to, v * E + e, g[e]);
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (first + e >= 0 && first + e < classes) Vec<T>::put(to, first + e, g[e]);
             }
         }
     }
@@ -443,14 +576,14 @@ void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &
            sums, keys);
     if (s.splits == 1) return;
     if (!cx.launch(K_LOGPROB, 0.0)) return;
-    cx.run(logprob_join_k<T>, dim3((unsigned)x.rows), dim3(64), 0, p, x.ld, x.classes, s.splits, labels, out, sums, keys);
+    cx.run(logprob_join_k<T>, dim3((unsigned)x.rows), dim3(kThreads), 0, p, x.ld, x.classes, s.splits, labels, out, sums, keys);
 }
 
 template <typename T>
 void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,
               const float *d_entropy, float scale, T *out, int64_t out_ld) {
     if (!cx.launch(K_LOGPROB, (double)x.rows * (2.0 * x.classes * sizeof(T) + 16.0), 8.0 * (double)x.rows * x.classes)) return;
-    const int vecs = (x.classes + Vec<T>::E - 1) / Vec<T>::E;
+    const int vecs = (x.classes + 2 * Vec<T>::E - 2) / Vec<T>::E;  // (of a row that starts anywhere in its first vector)
     int tshift = 0;
     while (tshift < 8 && (kFly << tshift) < vecs) ++tshift;
     const int64_t groups = (x.rows + (kThreads >> tshift) - 1) / (kThreads >> tshift);
