@@ -11,9 +11,9 @@
 // Top classes.  Classes are ordered by one 64-bit key: the value's bits made monotonic, above the complement of the class
 // number, so that no two are equal.  Every thread of a row knows the largest value of its own vectors; the top_k-th largest
 // of these (to 16 bits, by bisection: count the threads at or above a bit pattern) bounds the top_k-th largest class from
-// below.  The few classes at or above the bound are listed -- a thread reads again only the group of vectors that holds its
-// largest, or all of its own where a second group reaches the bound -- and each takes the place that the number of larger keys
-// in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
+// below.  The few classes at or above the bound are listed -- from the group of vectors that holds a thread's largest, which
+// it has kept in registers, or by reading the thread's vectors again where a second group reaches the bound -- and each takes
+// the place that the number of larger keys in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
 // wavefront takes its largest keys one by one and the lists are merged.
 #include "kernels.h"
 
@@ -22,7 +22,6 @@ namespace rvn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kFly = 4;  // vectors a thread requests before it uses the first
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
 constexpr float kLowest = -3.402823466e38f;
 
@@ -33,7 +32,7 @@ template <typename T>
 struct Vec;  // 16 bytes of a row as fp32 values, and back
 template <>
 struct Vec<float> {
-    static constexpr int E = 4;
+    static constexpr int E = 4, FLY = 4;  // FLY: vectors a thread requests before it uses the first
     static __device__ __forceinline__ float one(const void *p, int64_t i) { return static_cast<const float *>(p)[i]; }
     static __device__ __forceinline__ void widen(u4 w, float (&v)[E]) {
 #pragma unroll
@@ -49,7 +48,7 @@ struct Bf16 {
 };
 template <>
 struct Vec<Bf16> {
-    static constexpr int E = 8;
+    static constexpr int E = 8, FLY = 2;
     static __device__ __forceinline__ float one(const void *p, int64_t i) {
         return __uint_as_float((uint32_t)static_cast<const uint16_t *>(p)[i] << 16);
     }
@@ -96,7 +95,7 @@ __device__ __forceinline__ int skew_of(const T *p) {
 }
 
 // Bits that order as the values do, -0 as 0, NaN above all; never 0, and never 0xffffffff, which is above every key.
-constexpr uint32_t kNanOrder = 0xff800001u;
+constexpr uint32_t kNanOrder = 0xff800001u, kLowestOrder = 0x007fffffu;  // (of -infinity)
 __device__ __forceinline__ uint32_t order_bits(float x) {
     if (x != x) return kNanOrder;
     const uint32_t b = __float_as_uint(x + 0.f);
@@ -157,7 +156,7 @@ struct Part {
 };
 
 template <typename T>
-__device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T>::E], float most) {
+__device__ __forceinline__ void add_values(Sums &a, const float (&x)[Vec<T>::FLY][Vec<T>::E], float most) {
     constexpr int E = Vec<T>::E;
     const float m = fmaxf(a.m, most);
     const float down = (a.m - m) * kLog2e, f = __builtin_amdgcn_exp2f(down);
@@ -165,7 +164,7 @@ __device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T
     a.s *= f;
     a.m = m;
 #pragma unroll
-    for (int u = 0; u < kFly; ++u)
+    for (int u = 0; u < Vec<T>::FLY; ++u)
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             const float d = (x[u][e] - m) * kLog2e, w = __builtin_amdgcn_exp2f(d);
@@ -174,42 +173,62 @@ __device__ __forceinline__ void add_values(Sums &a, const float (&x)[kFly][Vec<T
         }
 }
 
-// The largest value of a thread's vectors, the first group of kFly vectors that holds it, and the largest of the others.
+// The largest value of a thread's vectors, the first group of vectors that holds it and what it holds, and the largest
+// value of the others.
+template <int FLY>
 struct Top {
     float value, second;
     int group;
+    u4 kept[FLY];
 };
 
-template <typename T>
-__device__ __forceinline__ Sums stream(const Part<T> &p, int thread, Top &top) {
+// TOP: fills `top` (else it is not looked at).
+template <bool TOP, typename T>
+__device__ __forceinline__ Sums stream(const Part<T> &p, int thread, Top<Vec<T>::FLY> &top) {
     constexpr int E = Vec<T>::E;
     Sums a{kLowest, 0.f, 0.f};
-    top = Top{-INFINITY, -INFINITY, 0};
-    for (int g = 0; thread + g * kFly * p.NT < p.vecs; ++g) {
-        float x[kFly][E];
-        const int v0 = thread + g * kFly * p.NT;
-        if (p.at(v0) >= 0 && p.at(v0 + (kFly - 1) * p.NT) + E <= p.length) {
+    if constexpr (TOP) {
+        top.value = top.second = -INFINITY;
+        top.group = 0;
 #pragma unroll
-            for (int u = 0; u < kFly; ++u) Vec<T>::widen(*reinterpret_cast<const u4_any *>(p.row + p.at(v0 + u * p.NT)), x[u]);
+        for (int u = 0; u < Vec<T>::FLY; ++u) top.kept[u] = u4{0u, 0u, 0u, 0u};
+    }
+    for (int g = 0; thread + g * Vec<T>::FLY * p.NT < p.vecs; ++g) {
+        float x[Vec<T>::FLY][E];
+        u4 raw[Vec<T>::FLY];
+        const int v0 = thread + g * Vec<T>::FLY * p.NT;
+        if (p.at(v0) >= 0 && p.at(v0 + (Vec<T>::FLY - 1) * p.NT) + E <= p.length) {
+#pragma unroll
+            for (int u = 0; u < Vec<T>::FLY; ++u) raw[u] = *reinterpret_cast<const u4_any *>(p.row + p.at(v0 + u * p.NT));
         } else {
 #pragma unroll
-            for (int u = 0; u < kFly; ++u) {
+            for (int u = 0; u < Vec<T>::FLY; ++u) {
                 if (v0 + u * p.NT < p.vecs) {
                     load_vec(p.row, p.at(v0 + u * p.NT), p.length, x[u]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[u][e] = -INFINITY;
                 }
+                raw[u] = Vec<T>::narrow(x[u]);  // (exact: these were the type's own values)
             }
         }
+#pragma unroll
+        for (int u = 0; u < Vec<T>::FLY; ++u) Vec<T>::widen(raw[u], x[u]);
         float most = x[0][0];
 #pragma unroll
-        for (int u = 0; u < kFly; ++u)
+        for (int u = 0; u < Vec<T>::FLY; ++u)
 #pragma unroll
             for (int e = 0; e < E; ++e) most = fmaxf(most, x[u][e]);
-        const bool up = most > top.value;
-        top.second = fmaxf(top.second, up ? top.value : most);
-        if (up) top.value = most, top.group = g;
+        if constexpr (TOP) {
+            const bool up = g == 0 || most > top.value;
+            if (g > 0) top.second = fmaxf(top.second, up ? top.value : most);
+            top.value = up ? most : top.value;
+            top.group = up ? g : top.group;
+#pragma unroll
+            for (int u = 0; u < Vec<T>::FLY; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top.kept[u][i] = up ? raw[u][i] : top.kept[u][i];
+        }
         add_values<T>(a, x, most);
     }
     return a;
@@ -232,27 +251,23 @@ __device__ __forceinline__ void team_barrier() {
     else __syncthreads();
 }
 
-// Lists the classes of vector v whose order bits reach `bound`.
+// Lists the classes of vector v, which holds x, whose values reach `least`.
 template <typename T>
-__device__ __forceinline__ void list_vector(const Part<T> &p, int v, uint32_t bound, Key *list, int *listed) {
-    constexpr int E = Vec<T>::E;
-    float x[E];
-    load_vec(p.row, p.at(v), p.length, x);
+__device__ __forceinline__ void list_values(const Part<T> &p, int v, const float (&x)[Vec<T>::E], float least, Key *list, int *listed) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const uint32_t order = order_bits(x[e]);
+    for (int e = 0; e < Vec<T>::E; ++e) {
+        if (!(x[e] >= least)) continue;
         const int i = p.at(v) + e;
-        if (order >= bound && i >= 0 && i < p.length) {
-            const int slot = atomicAdd(listed, 1);
-            if (slot < kListed) list[slot] = Key{order, 0xffffffffu - (uint32_t)(p.first + i)};
-        }
+        if (i < 0 || i >= p.length) continue;
+        const int slot = atomicAdd(listed, 1);
+        if (slot < kListed) list[slot] = Key{order_bits(x[e]), 0xffffffffu - (uint32_t)(p.first + i)};
     }
 }
 
 // Fills lds.list with lds.listed keys among which are the part's top_k largest (or all that it has).  More than kListed:
 // the list is not complete.  The part holds no NaN.  All threads of the team call it; the last barrier is the caller's.
 template <typename T, int NW>
-__device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top &top, int top_k, TeamLds<NW> &lds) {
+__device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top<Vec<T>::FLY> &top, int top_k, TeamLds<NW> &lds) {
     const bool has = thread < p.vecs;
     const uint32_t mine = has ? order_bits(top.value) : 0u;
     uint32_t seen[NW];
@@ -274,15 +289,27 @@ __device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top
         for (int w = 0; w < NW; ++w) count += __popcll(__ballot(seen[w] >= next));
         if (count >= top_k) bound = next;
     }
-    if (has && mine >= bound) {
-        const bool all = order_bits(top.second) >= bound;
-        const int g0 = all ? 0 : top.group, g1 = all ? (p.vecs + kFly * p.NT - 1) / (kFly * p.NT) : top.group + 1;
-        for (int g = g0; g < g1; ++g)
+    const float least = bound <= kLowestOrder ? -INFINITY : value_of(bound);  // order bits reach `bound`: the value reaches this
+    // A thread whose largest reaches the bound lists what it kept; where its second group reaches it too, the wavefront reads
+    // all vectors of that thread, one a lane.
+    const bool reaches = has && mine >= bound, all = reaches && order_bits(top.second) >= bound && p.vecs > Vec<T>::FLY * p.NT;
+    if (reaches && !all) {
 #pragma unroll
-            for (int u = 0; u < kFly; ++u) {
-                const int v = thread + (g * kFly + u) * p.NT;
-                if (v < p.vecs) list_vector(p, v, bound, lds.list, &lds.listed);
-            }
+        for (int u = 0; u < Vec<T>::FLY; ++u) {
+            const int v = thread + (top.group * Vec<T>::FLY + u) * p.NT;
+            float x[Vec<T>::E];
+            Vec<T>::widen(top.kept[u], x);
+            if (v < p.vecs) list_values(p, v, x, least, lds.list, &lds.listed);
+        }
+    }
+    const int lane = thread & 63;
+    for (unsigned long long left = __ballot(all); left; left &= left - 1) {
+        const int owner = thread - lane + __ffsll(left) - 1;
+        for (int v = owner + lane * p.NT; v < p.vecs; v += 64 * p.NT) {
+            float x[Vec<T>::E];
+            load_vec(p.row, p.at(v), p.length, x);
+            list_values(p, v, x, least, lds.list, &lds.listed);
+        }
     }
 }
 
@@ -356,7 +383,7 @@ __device__ __forceinline__ void merge_lists(const Key *keys, int lists, int top_
 // place(r, key) for the r-th largest class of the part, r < top_k ({0, 0} where the part has fewer).  nan: the part holds
 // one.  All threads of the team call it, with the same nan.
 template <typename T, int NW, typename Place>
-__device__ __forceinline__ void team_top(const Part<T> &p, int thread, const Top &top, bool nan, int top_k, TeamLds<NW> &lds, Place place) {
+__device__ __forceinline__ void team_top(const Part<T> &p, int thread, const Top<Vec<T>::FLY> &top, bool nan, int top_k, TeamLds<NW> &lds, Place place) {
     if (!nan) {
         list_top(p, thread, top, top_k, lds);
         team_barrier<NW>();
@@ -405,7 +432,7 @@ __device__ __forceinline__ void put_top(const LogprobOut &out, int64_t at, int r
 }
 
 // One wavefront per row, for short rows; four rows to a workgroup.
-template <typename T>
+template <typename T, bool TOP>
 __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t rows, int64_t ld, int classes, const int64_t *labels,
                                                            const LogprobOut out) {
     __shared__ TeamLds<1> lds[kThreads / 64];
@@ -413,17 +440,18 @@ __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t r
     const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + wave;
     if (at >= rows) return;
     const Part<T> p(x + at * ld, 0, classes, 64);
-    Top top;
-    const Sums a = wave_join(stream(p, lane, top));
+    Top<Vec<T>::FLY> top;
+    const Sums a = wave_join(stream<TOP>(p, lane, top));
     if (lane == 0) put_row(p.row, classes, at, a, labels, out);
-    if (out.top_k == 0) return;
-    const Row row = row_of(a);
-    team_top<T, 1>(p, lane, top, row.nan, out.top_k, lds[wave], [&](int i, Key k) { put_top(out, at, i, k, row); });
+    if constexpr (TOP) {
+        const Row row = row_of(a);
+        team_top<T, 1>(p, lane, top, row.nan, out.top_k, lds[wave], [&](int i, Key k) { put_top(out, at, i, k, row); });
+    }
 }
 
 // A workgroup of NW wavefronts per part of a row.  splits == 1: the whole row, results written here.  Otherwise the
 // part's sums and list go to `sums` and `keys` ([row][split]) for logprob_join_k.
-template <typename T, int NW>
+template <typename T, int NW, bool TOP>
 __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t ld, int classes, int splits, int share,
                                                            const int64_t *labels, const LogprobOut out, float4 *sums, Key *keys) {
     __shared__ TeamLds<NW> lds;
@@ -434,8 +462,8 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t l
     const int first = split * share;
     const T *row = x + at * ld;
     const Part<T> p(row + first, first, min(share, classes - first), NW * 64);
-    Top top;
-    const Sums mine = wave_join(stream(p, thread, top));
+    Top<Vec<T>::FLY> top;
+    const Sums mine = wave_join(stream<TOP>(p, thread, top));
     if (lane == 0) parts[wave] = mine;
     __syncthreads();
     Sums a = parts[0];
@@ -446,12 +474,13 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t l
         if (splits == 1) put_row(row, classes, at, a, labels, out);
         else sums[slot] = make_float4(a.m, a.s, a.t, 0.f);
     }
-    if (out.top_k == 0) return;
-    const Row r = row_of(a);
-    team_top<T, NW>(p, thread, top, r.nan, out.top_k, lds, [&](int i, Key k) {
-        if (splits == 1) put_top(out, at, i, k, r);
-        else keys[slot * out.top_k + i] = k;
-    });
+    if constexpr (TOP) {
+        const Row r = row_of(a);
+        team_top<T, NW>(p, thread, top, r.nan, out.top_k, lds, [&](int i, Key k) {
+            if (splits == 1) put_top(out, at, i, k, r);
+            else keys[slot * out.top_k + i] = k;
+        });
+    }
 }
 
 // Joins the parts (at most 64) of a row.  A part's last key bounds the row's top_k-th from below; what reaches the largest
@@ -490,7 +519,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_k(const T *x, int64_t l
 
 // ---- gradient ------------------------------------------------------------------------------------------------
 
-// 2^tshift neighbouring threads share a row; blockIdx.x counts pieces of kFly vectors a thread, blockIdx.y groups of rows.
+// 2^tshift neighbouring threads share a row; blockIdx.x counts pieces of FLY vectors a thread, blockIdx.y groups of rows.
 template <typename T>
 __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t rows, int64_t ld, int classes, int tshift,
                                                           const int64_t *labels, const float *lse, const float *entropy,
@@ -498,7 +527,7 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
                                                           int64_t out_ld) {
     constexpr int E = Vec<T>::E;
     const int team = 1 << tshift, per_block = kThreads >> tshift;
-    const int v0 = (int)blockIdx.x * team * kFly + ((int)threadIdx.x & (team - 1));
+    const int v0 = (int)blockIdx.x * team * Vec<T>::FLY + ((int)threadIdx.x & (team - 1));
     for (int64_t at = (int64_t)blockIdx.y * per_block + ((int)threadIdx.x >> tshift); at < rows; at += (int64_t)gridDim.y * per_block) {
         const T *row = x + at * ld;
         T *to = out + at * out_ld;
@@ -511,7 +540,7 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
         // a term whose weight is 0 is absent, whatever the row holds; so is every term of a row that has no class
         const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
 #pragma unroll
-        for (int u = 0; u < kFly; ++u) {
+        for (int u = 0; u < Vec<T>::FLY; ++u) {
             const int v = v0 + u * team, first = v * E - skew;
             if (v >= vecs) break;
             float g[E];
@@ -567,13 +596,14 @@ void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &
     if (!cx.launch(K_LOGPROB, bytes, 5.0 * (double)x.rows * x.classes)) return;
     if (s.wave) {
         const int per = kThreads / 64;
-        cx.run(logprob_wave_k<T>, dim3((unsigned)((x.rows + per - 1) / per)), dim3(kThreads), 0, p, x.rows, x.ld, x.classes, labels, out);
+        cx.run(out.top_k ? logprob_wave_k<T, true> : logprob_wave_k<T, false>, dim3((unsigned)((x.rows + per - 1) / per)), dim3(kThreads), 0, p,
+               x.rows, x.ld, x.classes, labels, out);
         return;
     }
     float4 *sums = static_cast<float4 *>(scratch);
     Key *keys = reinterpret_cast<Key *>(sums + (s.splits > 1 ? x.rows * s.splits : 0));
-    cx.run(logprob_block_k<T, 4>, dim3((unsigned)(x.rows * s.splits)), dim3(256), 0, p, x.ld, x.classes, s.splits, s.share, labels, out,
-           sums, keys);
+    cx.run(out.top_k ? logprob_block_k<T, 4, true> : logprob_block_k<T, 4, false>, dim3((unsigned)(x.rows * s.splits)), dim3(256), 0, p, x.ld,
+           x.classes, s.splits, s.share, labels, out, sums, keys);
     if (s.splits == 1) return;
     if (!cx.launch(K_LOGPROB, 0.0)) return;
     cx.run(logprob_join_k<T>, dim3((unsigned)x.rows), dim3(kThreads), 0, p, x.ld, x.classes, s.splits, labels, out, sums, keys);
@@ -585,9 +615,9 @@ void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse,
     if (!cx.launch(K_LOGPROB, (double)x.rows * (2.0 * x.classes * sizeof(T) + 16.0), 8.0 * (double)x.rows * x.classes)) return;
     const int vecs = (x.classes + 2 * Vec<T>::E - 2) / Vec<T>::E;  // (of a row that starts anywhere in its first vector)
     int tshift = 0;
-    while (tshift < 8 && (kFly << tshift) < vecs) ++tshift;
+    while (tshift < 8 && (Vec<T>::FLY << tshift) < vecs) ++tshift;
     const int64_t groups = (x.rows + (kThreads >> tshift) - 1) / (kThreads >> tshift);
-    const dim3 grid((unsigned)((vecs + (kFly << tshift) - 1) / (kFly << tshift)), (unsigned)(groups < 65535 ? groups : 65535));
+    const dim3 grid((unsigned)((vecs + (Vec<T>::FLY << tshift) - 1) / (Vec<T>::FLY << tshift)), (unsigned)(groups < 65535 ? groups : 65535));
     cx.run(logprob_bwd_k<T>, grid, dim3(kThreads), 0, static_cast<const T *>(x.p), x.rows, x.ld, x.classes, tshift, labels, lse, entropy,
            d_logprob, d_entropy, scale, out, out_ld);
 }
