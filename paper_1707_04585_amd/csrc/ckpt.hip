@@ -40,50 +40,68 @@ __device__ __forceinline__ f4 decode(uint32_t q, float s) {
     return v;
 }
 
-// 2^tshift neighbouring lanes share a group (128 pixels, or a whole smaller plane); blockIdx.x counts the groups of an
-// image, blockIdx.y the images.
+// 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
+// pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
+// requests the quads of kFly images before it uses the first.
 template <bool BN>
 __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict__ x, int64_t sn, int64_t sc, int N, int C, int HW,
                                                         int G, FastDiv by_g, int tshift, const float *__restrict__ stats,
                                                         int8_t *__restrict__ q, float *__restrict__ s) {
+    constexpr int kFly = 2;
     const int item = (int)blockIdx.x * (kThreads >> tshift) + ((int)threadIdx.x >> tshift), lane = (int)threadIdx.x & ((1 << tshift) - 1);
     const bool live = item < C * G;
     const int ch = live ? quotient(item, by_g) : 0, group = live ? item - ch * G : 0;
-    const int i = group * kCkptGroup + lane * 4, left = HW - i;
-    const bool mine = live && left > 0;
+    const int i = group * kCkptGroup + lane * 4;
+    const int left[2] = {live ? HW - i : 0, live && tshift == 4 ? HW - i - 64 : 0};
     float scale = 0.f, shift = 0.f;
     if (BN) scale = stats[2 * C + ch], shift = stats[3 * C + ch];
-    for (int n = (int)blockIdx.y; n < N; n += (int)gridDim.y) {
-        f4 v = {0.f, 0.f, 0.f, 0.f};
-        if (mine) v = load4(x + (int64_t)n * sn + (int64_t)ch * sc + i, left);
-        // magnitudes as bit patterns: these order as the values do, infinities and NaN on top
-        uint32_t most = max(max(__float_as_uint(v.x) & 0x7fffffffu, __float_as_uint(v.y) & 0x7fffffffu),
-                            max(__float_as_uint(v.z) & 0x7fffffffu, __float_as_uint(v.w) & 0x7fffffffu));
-        for (int o = 1 << tshift >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
-        if (!mine) continue;
-        const bool finite = most < 0x7f800000u;
-        const float a = fmaxf(finite ? __uint_as_float(most) : 1.f, kLeast);
-        const float step = a / kTop, inverse = kTop / a;
-        uint32_t word = 0;
-        if (finite) {
+    const float *px = x + (int64_t)ch * sc + i;
+    for (int n0 = (int)blockIdx.y * kFly; n0 < N; n0 += (int)gridDim.y * kFly) {
+        f4 v[kFly][2];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float c = rintf(v[j] * inverse);
-                if (BN) {
-                    const bool want = fmaf(v[j], scale, shift) > 0.f, got = fmaf(c * step, scale, shift) > 0.f;
-                    if (want != got) c += (scale > 0.f) == want ? 1.f : -1.f;
-                }
-                word |= ((uint32_t)(int)c & 0xffu) << (8 * j);
+        for (int u = 0; u < kFly; ++u)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v[u][h] = f4{0.f, 0.f, 0.f, 0.f};
+                if (n0 + u < N && left[h] > 0) v[u][h] = load4(px + (int64_t)(n0 + u) * sn + h * 64, left[h]);
             }
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            if (n0 + u >= N) break;  // (uniform)
+            // magnitudes as bit patterns: these order as the values do, infinities and NaN on top
+            uint32_t most = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) most = max(most, __float_as_uint(v[u][h][j]) & 0x7fffffffu);
+            for (int o = 1 << tshift >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+            const bool finite = most < 0x7f800000u;
+            const float a = fmaxf(finite ? __uint_as_float(most) : 1.f, kLeast);
+            const float step = a / kTop, inverse = finite ? kTop / a : 0.f;
+            const int64_t plane = (int64_t)(n0 + u) * C + ch;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (left[h] <= 0) continue;
+                uint32_t word = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float c = rintf(v[u][h][j] * inverse);
+                    if (BN) {
+                        const bool want = fmaf(v[u][h][j], scale, shift) > 0.f, got = fmaf(c * step, scale, shift) > 0.f;
+                        if (want != got) c += (scale > 0.f) == want ? 1.f : -1.f;
+                    }
+                    word |= ((uint32_t)(int)c & 0xffu) << (8 * j);
+                }
+                if (!finite) word = 0;
+                int8_t *out = q + plane * HW + i + h * 64;
+                if (left[h] >= 4) {
+                    *reinterpret_cast<u32_any *>(out) = word;
+                } else {
+                    for (int j = 0; j < left[h]; ++j) out[j] = (int8_t)(word >> (8 * j));
+                }
+            }
+            if (live && lane == 0) s[plane * G + group] = finite ? step : __uint_as_float(0x7fc00000u);
         }
-        const int64_t plane = (int64_t)n * C + ch;
-        int8_t *out = q + plane * HW + i;
-        if (left >= 4) {
-            *reinterpret_cast<u32_any *>(out) = word;
-        } else {
-            for (int j = 0; j < left; ++j) out[j] = (int8_t)(word >> (8 * j));
-        }
-        if (lane == 0) s[plane * G + group] = finite ? step : __uint_as_float(0x7fc00000u);
     }
 }
 
@@ -109,14 +127,43 @@ struct BnLayer {
     FastDiv by_per;  // quads of a plane
 };
 
-// dz and xh of one quad of channel ch (pixels beyond the plane's end: zero)
-__device__ __forceinline__ void quad(const BnLayer &b, uint32_t word, float step, f4 da, int left, float mean, float rstd, float scale,
-                                     float shift, f4 &dz, f4 &xh) {
-    const f4 v = decode(word, step);
+// A channel's constants, and the quads of its planes: quad e of N * per.
+struct Channel {
+    float mean, rstd, scale, shift;
+};
+__device__ __forceinline__ Channel channel(const BnLayer &b, int ch) {
+    return Channel{b.stats[ch], b.stats[b.C + ch], b.stats[2 * b.C + ch], b.stats[3 * b.C + ch]};
+}
+struct Place {
+    int n, i, left;
+    int64_t plane;
+};
+__device__ __forceinline__ Place place(const BnLayer &b, int ch, int e) {
+    const int n = quotient(e, b.by_per), i = (e - n * (int)b.by_per.d) * 4;
+    return Place{n, i, b.HW - i, (int64_t)n * b.C + ch};
+}
+// What a quad is made of; zeros where `live` is false.
+struct Quad {
+    uint32_t word;
+    float step;
+    f4 da;
+};
+__device__ __forceinline__ Quad fetch(const BnLayer &b, const Place &at, int ch, bool live, const float *da, int64_t dsn, int64_t dsc) {
+    Quad q{0u, 0.f, f4{0.f, 0.f, 0.f, 0.f}};
+    if (live) {
+        q.word = load_codes(b.q + at.plane * b.HW + at.i, at.left);
+        q.step = b.s[at.plane * b.G + at.i / kCkptGroup];
+        q.da = load4(da + (int64_t)at.n * dsn + (int64_t)ch * dsc + at.i, at.left);
+    }
+    return q;
+}
+// dz and x - mean (pixels that do not exist: dz is zero, as their da is)
+__device__ __forceinline__ void quad(const Quad &q, const Channel &c, f4 &dz, f4 &xm) {
+    const f4 v = decode(q.word, q.step);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        dz[j] = j < left && fmaf(v[j], scale, shift) > 0.f ? da[j] : 0.f;
-        xh[j] = (v[j] - mean) * rstd;
+        dz[j] = fmaf(v[j], c.scale, c.shift) > 0.f ? q.da[j] : 0.f;
+        xm[j] = v[j] - c.mean;
     }
 }
 
@@ -134,26 +181,33 @@ __device__ __forceinline__ void put_quad(f4 r, int left, float *po, uint16_t *p1
     }
 }
 
-// sums[ch][split] = (sum dz, sum dz * xh) over a share of a channel's quads; threads add in fp32 (at most a few hundred
-// terms each), everything above in double
+constexpr int kFly = 4;  // quads a thread requests before it uses the first
+
+// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads add in fp32 (at most a few
+// hundred terms each), everything above in double
 __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, int share,
                                                              double2 *sums) {
     __shared__ double part[4][2];
-    const int ch = (int)blockIdx.y, per = (int)b.by_per.d, total = b.N * per;
+    const int ch = (int)blockIdx.y, total = b.N * (int)b.by_per.d;
     const int first = (int)blockIdx.x * share, last = min(total, first + share);
-    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
+    const Channel c = channel(b, ch);
     float a0 = 0.f, a1 = 0.f;
-    for (int e = first + (int)threadIdx.x; e < last; e += kThreads) {
-        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
-        const int64_t plane = (int64_t)n * b.C + ch;
-        const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
-        const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
-        f4 dz, xh;
-        quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz, xh);
+    for (int e0 = first + (int)threadIdx.x; e0 < last; e0 += kFly * kThreads) {
+        Quad q[kFly];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            a0 += dz[j];
-            a1 = fmaf(dz[j], xh[j], a1);
+        for (int u = 0; u < kFly; ++u) {
+            const int e = e0 + u * kThreads;
+            q[u] = fetch(b, place(b, ch, e < last ? e : e0), ch, e < last, da, dsn, dsc);
+        }
+#pragma unroll
+        for (int u = 0; u < kFly; ++u) {
+            f4 dz, xm;
+            quad(q[u], c, dz, xm);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                a0 += dz[j];
+                a1 = fmaf(dz[j], xm[j], a1);
+            }
         }
     }
     const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
@@ -164,12 +218,25 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, co
             make_double2((part[0][0] + part[1][0]) + (part[2][0] + part[3][0]), (part[0][1] + part[1][1]) + (part[2][1] + part[3][1]));
 }
 
-__device__ __forceinline__ void put_sums(double sb, double sg, float *dgamma, float *dbeta, int ch, int accumulate) {
-    dbeta[ch] = (accumulate ? dbeta[ch] : 0.f) + (float)sb;
-    dgamma[ch] = (accumulate ? dgamma[ch] : 0.f) + (float)sg;
+// dx = scale * (dz - mean dz - xh * mean(dz * xh)) as scale * dz - a - (x - mean) * b
+struct Coefs {
+    float a, b;
+};
+__device__ __forceinline__ Coefs coefs(const Channel &c, double sum, double sum_xm, double inv_m) {
+    const double r = c.rstd, s = c.scale;
+    return Coefs{(float)(s * (sum * inv_m)), (float)(s * r * (r * sum_xm * inv_m))};
+}
+__device__ __forceinline__ f4 gradient(const f4 &dz, const f4 &xm, const Channel &c, const Coefs &k) {
+    f4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = fmaf(-xm[j], k.b, fmaf(c.scale, dz[j], -k.a));
+    return r;
 }
 
-constexpr int kApplyQuads = 4;  // a thread of the apply pass
+__device__ __forceinline__ void put_sums(const Channel &c, double sum, double sum_xm, float *dgamma, float *dbeta, int ch, int accumulate) {
+    dbeta[ch] = (accumulate ? dbeta[ch] : 0.f) + (float)sum;
+    dgamma[ch] = (accumulate ? dgamma[ch] : 0.f) + (float)(c.rstd * sum_xm);
+}
 
 // The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
 template <bool SKIP>
@@ -184,33 +251,34 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
         return;
     }
     const int bx = (int)blockIdx.x - carry.blocks, ch = quotient(bx, by_chunks), chunk = bx - ch * (int)by_chunks.d;
-    const int per = (int)b.by_per.d, total = b.N * per;
-    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
+    const int total = b.N * (int)b.by_per.d, e0 = chunk * kFly * kThreads + (int)threadIdx.x;
+    const Channel c = channel(b, ch);
+    Quad q[kFly];
+    f4 kv[kFly];
+#pragma unroll
+    for (int u = 0; u < kFly; ++u) {
+        const int e = e0 + u * kThreads;
+        const Place at = place(b, ch, e < total ? e : 0);
+        q[u] = fetch(b, at, ch, e < total, da, dsn, dsc);
+        if (SKIP && e < total) kv[u] = load4(skip + (int64_t)at.n * ksn + (int64_t)ch * ksc + at.i, at.left);
+    }
     // every wavefront adds the channel's partial sums for itself, in the same order
     const int lane = (int)threadIdx.x & 63;
     double2 p = make_double2(0.0, 0.0);
     if (lane < S) p = sums[(int64_t)ch * S + lane];
-    const double sb = wave_total(p.x), sg = wave_total(p.y);
-    if (chunk == 0 && threadIdx.x == 0) put_sums(sb, sg, dgamma, dbeta, ch, accumulate);
-    const float c1 = (float)(sb * inv_m), c2 = (float)(sg * inv_m);
+    const double sum = wave_total(p.x), sum_xm = wave_total(p.y);
+    if (chunk == 0 && threadIdx.x == 0) put_sums(c, sum, sum_xm, dgamma, dbeta, ch, accumulate);
+    const Coefs k = coefs(c, sum, sum_xm, inv_m);
 #pragma unroll
-    for (int k = 0; k < kApplyQuads; ++k) {
-        const int e = (chunk * kApplyQuads + k) * kThreads + (int)threadIdx.x;
+    for (int u = 0; u < kFly; ++u) {
+        const int e = e0 + u * kThreads;
         if (e >= total) return;
-        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
-        const int64_t plane = (int64_t)n * b.C + ch;
-        const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
-        const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
-        f4 dz, xh, kv = {0.f, 0.f, 0.f, 0.f};
-        if (SKIP) kv = load4(skip + (int64_t)n * ksn + (int64_t)ch * ksc + i, left);
-        quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz, xh);
-        f4 r;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            r[j] = scale * ((dz[j] - c1) - xh[j] * c2);
-            if (SKIP) r[j] += kv[j];
-        }
-        put_quad(r, left, out + (int64_t)n * osn + (int64_t)ch * osc + i, out16 ? out16 + plane * b.HW + i : nullptr);
+        const Place at = place(b, ch, e);
+        f4 dz, xm;
+        quad(q[u], c, dz, xm);
+        f4 r = gradient(dz, xm, c, k);
+        if (SKIP) r += kv[u];
+        put_quad(r, at.left, out + (int64_t)at.n * osn + (int64_t)ch * osc + at.i, out16 ? out16 + at.plane * b.HW + at.i : nullptr);
     }
 }
 
@@ -230,46 +298,36 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
         }
     }
     __shared__ double part[T / 64][2];
-    const int ch = (int)blockIdx.x - carry.blocks, per = (int)b.by_per.d, total = b.N * per;
-    const float mean = b.stats[ch], rstd = b.stats[b.C + ch], scale = b.stats[2 * b.C + ch], shift = b.stats[3 * b.C + ch];
-    f4 dz[kFusedQuads], xh[kFusedQuads];
+    const int ch = (int)blockIdx.x - carry.blocks, total = b.N * (int)b.by_per.d;
+    const Channel c = channel(b, ch);
+    f4 dz[kFusedQuads], xm[kFusedQuads];
     float a0 = 0.f, a1 = 0.f;
 #pragma unroll
-    for (int k = 0; k < kFusedQuads; ++k) {
-        const int e = (int)threadIdx.x + k * T;
-        dz[k] = f4{0.f, 0.f, 0.f, 0.f};
-        xh[k] = dz[k];
-        if (e < total) {
-            const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
-            const int64_t plane = (int64_t)n * b.C + ch;
-            const uint32_t word = load_codes(b.q + plane * b.HW + i, left);
-            const f4 dv = load4(da + (int64_t)n * dsn + (int64_t)ch * dsc + i, left);
-            quad(b, word, b.s[plane * b.G + i / kCkptGroup], dv, left, mean, rstd, scale, shift, dz[k], xh[k]);
-        }
+    for (int u = 0; u < kFusedQuads; ++u) {
+        const int e = (int)threadIdx.x + u * T;
+        quad(fetch(b, place(b, ch, e < total ? e : 0), ch, e < total, da, dsn, dsc), c, dz[u], xm[u]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            a0 += dz[k][j];
-            a1 = fmaf(dz[k][j], xh[k][j], a1);
+            a0 += dz[u][j];
+            a1 = fmaf(dz[u][j], xm[u][j], a1);
         }
     }
     const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = t0, part[threadIdx.x >> 6][1] = t1;
     __syncthreads();
-    double sb = 0.0, sg = 0.0;
+    double sum = 0.0, sum_xm = 0.0;
 #pragma unroll
-    for (int w = 0; w < T / 64; ++w) sb += part[w][0], sg += part[w][1];
-    if (threadIdx.x == 0) put_sums(sb, sg, dgamma, dbeta, ch, accumulate);
-    const float c1 = (float)(sb * inv_m), c2 = (float)(sg * inv_m);
+    for (int w = 0; w < T / 64; ++w) sum += part[w][0], sum_xm += part[w][1];
+    if (threadIdx.x == 0) put_sums(c, sum, sum_xm, dgamma, dbeta, ch, accumulate);
+    const Coefs k = coefs(c, sum, sum_xm, inv_m);
 #pragma unroll
-    for (int k = 0; k < kFusedQuads; ++k) {
-        const int e = (int)threadIdx.x + k * T;
+    for (int u = 0; u < kFusedQuads; ++u) {
+        const int e = (int)threadIdx.x + u * T;
         if (e >= total) return;
-        const int n = quotient(e, b.by_per), i = (e - n * per) * 4, left = b.HW - i;
-        f4 r;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = scale * ((dz[k][j] - c1) - xh[k][j] * c2);
-        if (SKIP) r += load4(skip + (int64_t)n * ksn + (int64_t)ch * ksc + i, left);
-        put_quad(r, left, out + (int64_t)n * osn + (int64_t)ch * osc + i, out16 ? out16 + ((int64_t)n * b.C + ch) * b.HW + i : nullptr);
+        const Place at = place(b, ch, e);
+        f4 r = gradient(dz[u], xm[u], c, k);
+        if (SKIP) r += load4(skip + (int64_t)at.n * ksn + (int64_t)ch * ksc + at.i, at.left);
+        put_quad(r, at.left, out + (int64_t)at.n * osn + (int64_t)ch * osc + at.i, out16 ? out16 + at.plane * b.HW + at.i : nullptr);
     }
 }
 
@@ -278,7 +336,7 @@ unsigned blocks_for(int64_t n, int per) { return (unsigned)((n + per - 1) / per)
 // Workgroups a channel's sums are split over: enough to fill the chip, at most one partial sum per lane.
 int ckpt_bn_splits(int c, const Geo &g) {
     const int64_t quads = (int64_t)g.n * quads_of(g.hw());
-    int64_t s = c >= 2048 ? 1 : 2048 / c;
+    int64_t s = c >= 8192 ? 1 : 8192 / c;
     s = s < 64 ? s : 64;
     const int64_t most = (quads + 2 * kThreads - 1) / (2 * kThreads);
     return (int)(s < most ? s : most);
@@ -290,9 +348,10 @@ void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k) {
     const int hw = g.hw(), G = ckpt_groups(hw);
     const double planes = (double)g.n * c;
     if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
-    int tshift = 0;  // lanes of a group: 32, or as many as a smaller plane has quads, rounded up to a power of two
-    while (tshift < 5 && (4 << tshift) < hw) ++tshift;
-    const dim3 grid(blocks_for((int64_t)c * G, kThreads >> tshift), (unsigned)(g.n < 65535 ? g.n : 65535));
+    int tshift = 0;  // lanes of a group: 16, or as many as a smaller plane has quads, rounded up to a power of two
+    while (tshift < 4 && (4 << tshift) < hw) ++tshift;
+    const int pairs = (g.n + 1) / 2;
+    const dim3 grid(blocks_for((int64_t)c * G, kThreads >> tshift), (unsigned)(pairs < 65535 ? pairs : 65535));
     if (stats)
         cx.run(ckpt_save_k<true>, grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
     else
@@ -344,7 +403,7 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
     if (cx.launch(K_BN_BWD_REDUCE, 5.0 * elems))
         cx.run(ckpt_bn_reduce_k, dim3((unsigned)S, (unsigned)c), dim3(kThreads), 0, b, da.p, da.sn, da.sc, share, sums);
     if (cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) {
-        const int chunks = (total + kApplyQuads * kThreads - 1) / (kApplyQuads * kThreads);
+        const int chunks = (total + kFly * kThreads - 1) / (kFly * kThreads);
         const dim3 grid((unsigned)(chunks * c + red.blocks));
         if (skip)
             cx.run(ckpt_bn_apply_k<true>, grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta,

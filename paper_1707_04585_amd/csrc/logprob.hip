@@ -73,25 +73,36 @@ struct Vec<Bf16> {
     }
 };
 
-// The vector that starts at class `at` (which may be up to E - 1 before the row's first) of a row of `classes`; what lies
-// outside the row reads as -infinity.
+// The vector that starts at class `at` (which may lie before the row's first) of `classes` of a row; what lies outside
+// these reads as -infinity.  Memory at classes lo .. hi - 1 of the row belongs to the matrix: a vector in there is read at
+// once and its outsiders dropped.
 template <typename T>
-__device__ __forceinline__ void load_vec(const T *row, int at, int classes, float (&v)[Vec<T>::E]) {
+__device__ __forceinline__ void load_vec(const T *row, int at, int classes, int lo, int hi, float (&v)[Vec<T>::E]) {
     constexpr int E = Vec<T>::E;
-    if (at >= 0 && at + E <= classes) {
+    if (at + E <= 0 || at >= classes) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = -INFINITY;
+    } else if (at >= lo && at + E <= hi) {
         Vec<T>::widen(*reinterpret_cast<const u4_any *>(row + at), v);
+        if (at < 0 || at + E > classes) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < classes ? v[e] : -INFINITY;
+        }
     } else {
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = at + e >= 0 && at + e < classes ? Vec<T>::one(row, at + e) : -INFINITY;
     }
 }
+// How far a matrix reaches before the first and behind the last class of row `at`, up to a cache line.
+__device__ __forceinline__ int reach(int64_t rows_away, int64_t ld) { return rows_away == 0 ? 0 : ld < 64 ? (int)ld : 64; }
 
-// Elements from the last 16-byte border to p: the vectors of a row start that much before it, so that their accesses are
-// aligned wherever the row begins.  (Rows of an odd number of bf16 logits, 4096 x 50021: 98.6 us with vectors from the row's
-// start, 77.5 where the rows are aligned by themselves.)
+// Elements from the last border to p: the vectors of a row start that much before it, so that their accesses are aligned
+// wherever the row begins; from 64 vectors on to whole cache lines, so that neighbouring workgroups write no line together.
+// (Rows of an odd number of bf16 logits: 4096 x 50021 in 98.6 us with vectors from the row's start, 86 on 16-byte borders.)
 template <typename T>
-__device__ __forceinline__ int skew_of(const T *p) {
-    return (int)((reinterpret_cast<uintptr_t>(p) & 15) / sizeof(T));
+__device__ __forceinline__ int skew_of(const T *p, int classes) {
+    const uintptr_t border = classes >= 64 * Vec<T>::E ? 128 : 16;
+    return (int)((reinterpret_cast<uintptr_t>(p) & (border - 1)) / sizeof(T));
 }
 
 // Bits that order as the values do, -0 as 0, NaN above all; never 0, and never 0xffffffff, which is above every key.
@@ -148,11 +159,13 @@ __device__ __forceinline__ Sums wave_join(Sums v) {
 template <typename T>
 struct Part {
     const T *row;  // at class `first`
-    int first, length, skew, vecs, NT;
-    __device__ __forceinline__ Part(const T *r, int f, int l, int nt) : row(r), first(f), length(l), skew(skew_of(r)), NT(nt) {
-        vecs = (l + skew + Vec<T>::E - 1) / Vec<T>::E;
-    }
+    int first, length, lo, hi, skew, vecs, NT;
+    // classes f .. f + l - 1 of row `at` of a matrix
+    __device__ __forceinline__ Part(const T *x, int64_t at, int64_t rows, int64_t ld, int classes, int f, int l, int nt)
+        : row(x + at * ld + f), first(f), length(l), lo(-f - reach(at, ld)), hi(classes - f + reach(rows - 1 - at, ld)),
+          skew(skew_of(row, l)), vecs((l + skew + Vec<T>::E - 1) / Vec<T>::E), NT(nt) {}
     __device__ __forceinline__ int at(int v) const { return v * Vec<T>::E - skew; }
+    __device__ __forceinline__ void load(int v, float (&x)[Vec<T>::E]) const { load_vec(row, at(v), length, lo, hi, x); }
 };
 
 template <typename T>
@@ -204,7 +217,7 @@ __device__ __forceinline__ Sums stream(const Part<T> &p, int thread, Top<Vec<T>:
 #pragma unroll
             for (int u = 0; u < Vec<T>::FLY; ++u) {
                 if (v0 + u * p.NT < p.vecs) {
-                    load_vec(p.row, p.at(v0 + u * p.NT), p.length, x[u]);
+                    p.load(v0 + u * p.NT, x[u]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < E; ++e) x[u][e] = -INFINITY;
@@ -307,7 +320,7 @@ __device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top
         const int owner = thread - lane + __ffsll(left) - 1;
         for (int v = owner + lane * p.NT; v < p.vecs; v += 64 * p.NT) {
             float x[Vec<T>::E];
-            load_vec(p.row, p.at(v), p.length, x);
+            p.load(v, x);
             list_values(p, v, x, least, lds.list, &lds.listed);
         }
     }
@@ -330,7 +343,7 @@ template <typename T>
 __device__ __forceinline__ Key best_below(const Part<T> &p, int v, Key below, Key best) {
     constexpr int E = Vec<T>::E;
     float x[E];
-    load_vec(p.row, p.at(v), p.length, x);
+    p.load(v, x);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int i = p.at(v) + e;
@@ -439,7 +452,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t r
     const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
     const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + wave;
     if (at >= rows) return;
-    const Part<T> p(x + at * ld, 0, classes, 64);
+    const Part<T> p(x, at, rows, ld, classes, 0, classes, 64);
     Top<Vec<T>::FLY> top;
     const Sums a = wave_join(stream<TOP>(p, lane, top));
     if (lane == 0) put_row(p.row, classes, at, a, labels, out);
@@ -452,7 +465,7 @@ __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t r
 // A workgroup of NW wavefronts per part of a row.  splits == 1: the whole row, results written here.  Otherwise the
 // part's sums and list go to `sums` and `keys` ([row][split]) for logprob_join_k.
 template <typename T, int NW, bool TOP>
-__global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t ld, int classes, int splits, int share,
+__global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t rows, int64_t ld, int classes, int splits, int share,
                                                            const int64_t *labels, const LogprobOut out, float4 *sums, Key *keys) {
     __shared__ TeamLds<NW> lds;
     __shared__ Sums parts[NW];
@@ -460,8 +473,7 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t l
     const int64_t at = splits == 1 ? (int64_t)blockIdx.x : (int64_t)(blockIdx.x / (unsigned)splits);
     const int split = splits == 1 ? 0 : (int)(blockIdx.x - (unsigned)at * (unsigned)splits);
     const int first = split * share;
-    const T *row = x + at * ld;
-    const Part<T> p(row + first, first, min(share, classes - first), NW * 64);
+    const Part<T> p(x, at, rows, ld, classes, first, min(share, classes - first), NW * 64);
     Top<Vec<T>::FLY> top;
     const Sums mine = wave_join(stream<TOP>(p, thread, top));
     if (lane == 0) parts[wave] = mine;
@@ -471,7 +483,7 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t l
     for (int w = 1; w < NW; ++w) a = join(a, parts[w]);
     const int64_t slot = at * splits + split;
     if (thread == 0) {
-        if (splits == 1) put_row(row, classes, at, a, labels, out);
+        if (splits == 1) put_row(p.row, classes, at, a, labels, out);
         else sums[slot] = make_float4(a.m, a.s, a.t, 0.f);
     }
     if constexpr (TOP) {
@@ -531,7 +543,7 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
     for (int64_t at = (int64_t)blockIdx.y * per_block + ((int)threadIdx.x >> tshift); at < rows; at += (int64_t)gridDim.y * per_block) {
         const T *row = x + at * ld;
         T *to = out + at * out_ld;
-        const int skew = skew_of(to), vecs = (classes + skew + E - 1) / E;
+        const int skew = skew_of(to, classes), vecs = (classes + skew + E - 1) / E;
         const int64_t label = labels ? labels[at] : RVN_NO_LABEL;
         const float norm = lse[at];
         float given = 0.f, spread = 0.f, h = 0.f;
@@ -539,30 +551,26 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
         if (d_entropy) spread = scale * d_entropy[at], h = entropy[at];
         // a term whose weight is 0 is absent, whatever the row holds; so is every term of a row that has no class
         const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
+        float g[Vec<T>::FLY][E];
+#pragma unroll
+        for (int u = 0; u < Vec<T>::FLY; ++u)
+            load_vec(row, (v0 + u * team) * E - skew, none ? 0 : classes, -reach(at, ld), classes + reach(rows - 1 - at, ld), g[u]);
 #pragma unroll
         for (int u = 0; u < Vec<T>::FLY; ++u) {
-            const int v = v0 + u * team, first = v * E - skew;
-            if (v >= vecs) break;
-            float g[E];
-            if (none) {
+            const int first = (v0 + u * team) * E - skew;
 #pragma unroll
-                for (int e = 0; e < E; ++e) g[e] = 0.f;
-            } else {
-                load_vec(row, first, classes, g);
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    const float logp = g[e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
-                    float d = -given * p;
-                    if (d_entropy) d -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
-                    g[e] = label == first + e ? d + given : d;
-                }
+            for (int e = 0; e < E; ++e) {
+                const float logp = g[u][e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
+                float d = -given * p;
+                if (d_entropy) d -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
+                g[u][e] = none ? 0.f : label == first + e ? d + given : d;
             }
             if (first >= 0 && first + E <= classes) {
-                *reinterpret_cast<u4 *>(to + first) = Vec<T>::narrow(g);
+                *reinterpret_cast<u4 *>(to + first) = Vec<T>::narrow(g[u]);
             } else {
 #pragma unroll
                 for (int e = 0; e < E; ++e)
-                    if (first + e >= 0 && first + e < classes) Vec<T>::put(to, first + e, g[e]);
+                    if (first + e >= 0 && first + e < classes) Vec<T>::put(to, first + e, g[u][e]);
             }
         }
     }
@@ -602,7 +610,7 @@ void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &
     }
     float4 *sums = static_cast<float4 *>(scratch);
     Key *keys = reinterpret_cast<Key *>(sums + (s.splits > 1 ? x.rows * s.splits : 0));
-    cx.run(out.top_k ? logprob_block_k<T, 4, true> : logprob_block_k<T, 4, false>, dim3((unsigned)(x.rows * s.splits)), dim3(256), 0, p, x.ld,
+    cx.run(out.top_k ? logprob_block_k<T, 4, true> : logprob_block_k<T, 4, false>, dim3((unsigned)(x.rows * s.splits)), dim3(256), 0, p, x.rows, x.ld,
            x.classes, s.splits, s.share, labels, out, sums, keys);
     if (s.splits == 1) return;
     if (!cx.launch(K_LOGPROB, 0.0)) return;
@@ -613,7 +621,8 @@ template <typename T>
 void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,
               const float *d_entropy, float scale, T *out, int64_t out_ld) {
     if (!cx.launch(K_LOGPROB, (double)x.rows * (2.0 * x.classes * sizeof(T) + 16.0), 8.0 * (double)x.rows * x.classes)) return;
-    const int vecs = (x.classes + 2 * Vec<T>::E - 2) / Vec<T>::E;  // (of a row that starts anywhere in its first vector)
+    // vectors of a row that starts anywhere between two borders (see skew_of)
+    const int border = (x.classes >= 64 * Vec<T>::E ? 128 : 16) / (int)sizeof(T), vecs = (x.classes + border - 1 + Vec<T>::E - 1) / Vec<T>::E;
     int tshift = 0;
     while (tshift < 8 && (Vec<T>::FLY << tshift) < vecs) ++tshift;
     const int64_t groups = (x.rows + (kThreads >> tshift) - 1) / (kThreads >> tshift);
