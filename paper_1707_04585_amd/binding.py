@@ -35,6 +35,13 @@ EXPORTS = [
     "revnet_head_workspace_bytes", "revnet_head_fwd", "revnet_head_bwd",
     "revnet_logprob_workspace_bytes", "revnet_logprob_fwd", "revnet_logprob_bwd",
 ]
+# Argument types of the entry points that small calls go through (p: address, z: size, l: int64, i: int32, f: float): with
+# them set ctypes converts plain numbers and byref() itself, which takes a fraction of wrapping each argument here.
+_SIGNATURES = {
+    "revnet_ckpt_save": "pppzp", "revnet_ckpt_load": "pzpp", "revnet_ckpt_bn_relu_bwd": "pzppppppipzp",
+    "revnet_head_fwd": "pppppzp", "revnet_head_bwd": "pppzppppipzp",
+    "revnet_logprob_fwd": "ppippppppzp", "revnet_logprob_bwd": "ppppppfpp",
+}
 STATIC_WS_BYTES = 32 << 20   # RVN_STATIC_WS_BYTES
 CKPT_GROUP = 128             # RVN_CKPT_GROUP
 NO_LABEL = -1                # RVN_NO_LABEL
@@ -125,6 +132,9 @@ def load_library():
         lib.revnet_last_error.restype = C.c_char_p
         for name in EXPORTS:
             getattr(lib, name)  # fail early if an entry point is missing
+        kinds = dict(p=C.c_void_p, z=C.c_size_t, l=C.c_int64, i=C.c_int32, f=C.c_float)
+        for name, args in _SIGNATURES.items():
+            getattr(lib, name).argtypes = [kinds[k] for k in args]
         _LIB = lib
     return _LIB
 
@@ -190,8 +200,8 @@ def _desc(d):
 def _tensor(t):
     if isinstance(t, rvn_tensor):
         return t
-    n, c, h, w = (int(v) for v in t.shape)
-    sn, sc, sh, sw = (int(v) for v in t.stride())
+    n, c, h, w = t.shape
+    sn, sc, sh, sw = t.stride()
     return rvn_tensor(t.data_ptr(), n, c, h, w, sn, sc, sh, sw)
 
 
@@ -267,8 +277,14 @@ def _tensor_array(ts):
     return arr
 
 
-def _is(t, dtype):
-    return str(t.dtype) == "torch." + dtype
+_DTYPE_NAMES = {}
+
+
+def _dtype_name(dtype):
+    name = _DTYPE_NAMES.get(dtype)
+    if name is None:
+        name = _DTYPE_NAMES[dtype] = str(dtype).rpartition(".")[2]
+    return name
 
 
 def _matrix(t, name):
@@ -278,7 +294,7 @@ def _matrix(t, name):
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"the columns of {name} must be contiguous")
-    dtype = F32 if _is(t, "float32") else BF16 if _is(t, "bfloat16") else -1
+    dtype = {"float32": F32, "bfloat16": BF16}.get(_dtype_name(t.dtype), -1)
     return rvn_matrix(t.data_ptr(), dtype, rows, cols, ld if rows > 1 else max(ld, cols))
 
 
@@ -286,7 +302,7 @@ def _vector(t, name, count, dtype="float32"):
     """Device pointer of a dense array of `count` elements (an integer is passed through as a pointer)."""
     if t is None or isinstance(t, int):
         return t
-    if not _is(t, dtype) or t.numel() != count or not t.is_contiguous():
+    if _dtype_name(t.dtype) != dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{name} must be {count} contiguous elements of {dtype}")
     return t.data_ptr()
 
@@ -560,15 +576,12 @@ def revnet_ckpt_bytes(n, c, h, w):
 def revnet_ckpt_save(x, stats, ckpt, stream=None):
     """stats: None, or a [4, c] tensor (mean, rstd, scale, shift)."""
     tx = _tensor(x)
-    kp, kb = _ws(ckpt)
-    _check(load_library().revnet_ckpt_save(C.byref(tx), C.c_void_p(_vector(stats, "stats", 4 * tx.c)), C.c_void_p(kp), C.c_size_t(kb),
-                                           C.c_void_p(_stream(stream))))
+    _check(load_library().revnet_ckpt_save(C.byref(tx), _vector(stats, "stats", 4 * tx.c), *_ws(ckpt), _stream(stream)))
 
 
 def revnet_ckpt_load(ckpt, x, stream=None):
     tx = _tensor(x)
-    kp, kb = _ws(ckpt)
-    _check(load_library().revnet_ckpt_load(C.c_void_p(kp), C.c_size_t(kb), C.byref(tx), C.c_void_p(_stream(stream))))
+    _check(load_library().revnet_ckpt_load(*_ws(ckpt), C.byref(tx), _stream(stream)))
 
 
 def revnet_ckpt_bn_relu_workspace_bytes(n, c, h, w):
@@ -580,12 +593,10 @@ def revnet_ckpt_bn_relu_workspace_bytes(n, c, h, w):
 def revnet_ckpt_bn_relu_bwd(ckpt, stats, da, skip, dx, d_gamma, d_beta, accumulate, ws, stream=None):
     ta, tx = _tensor(da), _tensor(dx)
     ts = None if skip is None else _tensor(skip)
-    kp, kb = _ws(ckpt)
-    wp, wb = _ws(ws)
+    c = ta.c
     _check(load_library().revnet_ckpt_bn_relu_bwd(
-        C.c_void_p(kp), C.c_size_t(kb), C.c_void_p(_vector(stats, "stats", 4 * ta.c)), C.byref(ta), _by_ref(ts), C.byref(tx),
-        C.c_void_p(_vector(d_gamma, "d_gamma", ta.c)), C.c_void_p(_vector(d_beta, "d_beta", ta.c)), C.c_int(int(accumulate)),
-        C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+        *_ws(ckpt), _vector(stats, "stats", 4 * c), C.byref(ta), _by_ref(ts), C.byref(tx), _vector(d_gamma, "d_gamma", c),
+        _vector(d_beta, "d_beta", c), int(accumulate), *_ws(ws), _stream(stream)))
 
 
 def revnet_stack_stored_bytes(desc, depth, n, h, w):
@@ -668,19 +679,14 @@ def revnet_head_workspace_bytes(desc, n, h, w):
 
 def revnet_head_fwd(desc, x, params, logits, saved, stream=None):
     d, p, tx, tl = _desc(desc), pack_head(params), _tensor(x), _matrix(logits, "logits")
-    sp, sb = _ws(saved)
-    _check(load_library().revnet_head_fwd(C.byref(d), C.byref(tx), C.byref(p), _by_ref(tl), C.c_void_p(sp), C.c_size_t(sb),
-                                          C.c_void_p(_stream(stream))))
+    _check(load_library().revnet_head_fwd(C.byref(d), C.byref(tx), C.byref(p), _by_ref(tl), *_ws(saved), _stream(stream)))
 
 
 def revnet_head_bwd(desc, x, saved, d_logits, params, dx, grads, accumulate_wgrads, ws, stream=None):
     d, p, g = _desc(desc), pack_head(params), pack_head(grads)
     tx, tl, td = _tensor(x), _matrix(d_logits, "d_logits"), _tensor(dx)
-    sp, sb = _ws(saved)
-    wp, wb = _ws(ws)
-    _check(load_library().revnet_head_bwd(C.byref(d), C.byref(tx), C.c_void_p(sp), C.c_size_t(sb), _by_ref(tl), C.byref(p), C.byref(td),
-                                          C.byref(g), C.c_int(int(accumulate_wgrads)), C.c_void_p(wp), C.c_size_t(wb),
-                                          C.c_void_p(_stream(stream))))
+    _check(load_library().revnet_head_bwd(C.byref(d), C.byref(tx), *_ws(saved), _by_ref(tl), C.byref(p), C.byref(td), C.byref(g),
+                                          int(accumulate_wgrads), *_ws(ws), _stream(stream)))
 
 
 def revnet_logprob_workspace_bytes(rows, classes, top_k):
@@ -695,21 +701,18 @@ def revnet_logprob_fwd(logits, labels, top_k, logprob, entropy, lse, top_ids, to
     rows = m.rows if m is not None else 0
     if top_k == 0:
         top_ids = top_logprob = None
-    wp, wb = _ws(ws)
     _check(load_library().revnet_logprob_fwd(
-        _by_ref(m), C.c_void_p(_vector(labels, "labels", rows, "int64")), C.c_int32(top_k),
-        C.c_void_p(_vector(logprob, "logprob", rows)), C.c_void_p(_vector(entropy, "entropy", rows)),
-        C.c_void_p(_vector(lse, "lse", rows)), C.c_void_p(_vector(top_ids, "top_ids", rows * top_k, "int64")),
-        C.c_void_p(_vector(top_logprob, "top_logprob", rows * top_k)), C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
+        _by_ref(m), _vector(labels, "labels", rows, "int64"), top_k, _vector(logprob, "logprob", rows), _vector(entropy, "entropy", rows),
+        _vector(lse, "lse", rows), _vector(top_ids, "top_ids", rows * top_k, "int64"), _vector(top_logprob, "top_logprob", rows * top_k),
+        *_ws(ws), _stream(stream)))
 
 
 def revnet_logprob_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, scale, d_logits, stream=None):
     m, d = _matrix(logits, "logits"), _matrix(d_logits, "d_logits")
     rows = m.rows if m is not None else 0
     _check(load_library().revnet_logprob_bwd(
-        _by_ref(m), C.c_void_p(_vector(labels, "labels", rows, "int64")), C.c_void_p(_vector(lse, "lse", rows)),
-        C.c_void_p(_vector(entropy, "entropy", rows)), C.c_void_p(_vector(d_logprob, "d_logprob", rows)),
-        C.c_void_p(_vector(d_entropy, "d_entropy", rows)), C.c_float(scale), _by_ref(d), C.c_void_p(_stream(stream))))
+        _by_ref(m), _vector(labels, "labels", rows, "int64"), _vector(lse, "lse", rows), _vector(entropy, "entropy", rows),
+        _vector(d_logprob, "d_logprob", rows), _vector(d_entropy, "d_entropy", rows), scale, _by_ref(d), _stream(stream)))
 
 
 def revnet_profile_begin():

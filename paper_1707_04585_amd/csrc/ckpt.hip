@@ -24,12 +24,23 @@ typedef uint32_t u32_any __attribute__((aligned(1)));
 typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
 typedef u16x4 u16x4_any __attribute__((aligned(2)));
 
-__device__ __forceinline__ uint32_t load_codes(const int8_t *p, int left) {
-    if (left >= 4) return *reinterpret_cast<const u32_any *>(p);
-    uint32_t v = (uint8_t)p[0];
-    if (left > 1) v |= (uint32_t)(uint8_t)p[1] << 8;
-    if (left > 2) v |= (uint32_t)(uint8_t)p[2] << 16;
+template <bool WHOLE>
+__device__ __forceinline__ uint32_t load_codes(const int8_t *plane, QuadAt q) {
+    if (WHOLE || q.end == 4) return *reinterpret_cast<const u32_any *>(plane + q.i);
+    uint32_t v = 0;
+#pragma unroll
+    for (int j = 0; j < 3; ++j) v |= j < q.end ? (uint32_t)(uint8_t)plane[j] << (8 * j) : 0u;
     return v;
+}
+template <bool WHOLE>
+__device__ __forceinline__ void store_codes(int8_t *plane, QuadAt q, uint32_t word) {
+    if (WHOLE || (q.from == 0 && q.end == 4)) {
+        *reinterpret_cast<u32_any *>(plane + q.i) = word;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (q.owns(j)) plane[q.i + j] = (int8_t)(word >> (8 * j));
 }
 __device__ __forceinline__ f4 decode(uint32_t q, float s) {
     f4 v;
@@ -43,7 +54,7 @@ __device__ __forceinline__ f4 decode(uint32_t q, float s) {
 // 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
 // pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
 // requests the quads of kFly images before it uses the first.
-template <bool BN>
+template <bool BN, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict__ x, int64_t sn, int64_t sc, int N, int C, int HW,
                                                         int G, FastDiv by_g, int tshift, const float *__restrict__ stats,
                                                         int8_t *__restrict__ q, float *__restrict__ s) {
@@ -51,11 +62,12 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
     const int item = (int)blockIdx.x * (kThreads >> tshift) + ((int)threadIdx.x >> tshift), lane = (int)threadIdx.x & ((1 << tshift) - 1);
     const bool live = item < C * G;
     const int ch = live ? quotient(item, by_g) : 0, group = live ? item - ch * G : 0;
-    const int i = group * kCkptGroup + lane * 4;
-    const int left[2] = {live ? HW - i : 0, live && tshift == 4 ? HW - i - 64 : 0};
+    const int k0 = group * (kCkptGroup / 4) + lane;
+    const QuadAt at[2] = {quad_at<WHOLE>(k0, HW), quad_at<WHOLE>(k0 + 16, HW)};
+    const bool mine[2] = {live && k0 * 4 < HW, live && tshift == 4 && (k0 + 16) * 4 < HW};
     float scale = 0.f, shift = 0.f;
     if (BN) scale = stats[2 * C + ch], shift = stats[3 * C + ch];
-    const float *px = x + (int64_t)ch * sc + i;
+    const float *px = x + (int64_t)ch * sc;
     for (int n0 = (int)blockIdx.y * kFly; n0 < N; n0 += (int)gridDim.y * kFly) {
         f4 v[kFly][2];
 #pragma unroll
@@ -63,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 v[u][h] = f4{0.f, 0.f, 0.f, 0.f};
-                if (n0 + u < N && left[h] > 0) v[u][h] = load4(px + (int64_t)(n0 + u) * sn + h * 64, left[h]);
+                if (n0 + u < N && mine[h]) v[u][h] = load4<WHOLE>(px + (int64_t)(n0 + u) * sn, at[h]);
             }
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
@@ -74,14 +86,14 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) most = max(most, __float_as_uint(v[u][h][j]) & 0x7fffffffu);
-            for (int o = 1 << tshift >> 1; o > 0; o >>= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+            most = team_most(most, tshift);
             const bool finite = most < 0x7f800000u;
             const float a = fmaxf(finite ? __uint_as_float(most) : 1.f, kLeast);
             const float step = a / kTop, inverse = finite ? kTop / a : 0.f;
             const int64_t plane = (int64_t)(n0 + u) * C + ch;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (left[h] <= 0) continue;
+                if (!mine[h]) continue;
                 uint32_t word = 0;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -93,12 +105,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
                     word |= ((uint32_t)(int)c & 0xffu) << (8 * j);
                 }
                 if (!finite) word = 0;
-                int8_t *out = q + plane * HW + i + h * 64;
-                if (left[h] >= 4) {
-                    *reinterpret_cast<u32_any *>(out) = word;
-                } else {
-                    for (int j = 0; j < left[h]; ++j) out[j] = (int8_t)(word >> (8 * j));
-                }
+                store_codes<WHOLE>(q + plane * HW, at[h], word);
             }
             if (live && lane == 0) s[plane * G + group] = finite ? step : __uint_as_float(0x7fc00000u);
         }
@@ -106,15 +113,17 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
 }
 
 // One lane per four pixels; blockIdx.x counts the quads of an image, blockIdx.y the images.
+template <bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_load_k(const int8_t *__restrict__ q, const float *__restrict__ s, int N, int C, int HW,
                                                         int G, FastDiv by_per, float *__restrict__ x, int64_t sn, int64_t sc) {
     const int per = (int)by_per.d, item = (int)blockIdx.x * kThreads + (int)threadIdx.x;
     if (item >= C * per) return;
-    const int ch = quotient(item, by_per), i = (item - ch * per) * 4, left = HW - i;
+    const int ch = quotient(item, by_per), k = item - ch * per;
+    const QuadAt at = quad_at<WHOLE>(k, HW);
     for (int n = (int)blockIdx.y; n < N; n += (int)gridDim.y) {
         const int64_t plane = (int64_t)n * C + ch;
-        const uint32_t word = load_codes(q + plane * HW + i, left);
-        store4(x + (int64_t)n * sn + (int64_t)ch * sc + i, left, decode(word, s[plane * G + i / kCkptGroup]));
+        const uint32_t word = load_codes<WHOLE>(q + plane * HW, at);
+        store4<WHOLE>(x + (int64_t)n * sn + (int64_t)ch * sc, at, decode(word, s[plane * G + k / (kCkptGroup / 4)]));
     }
 }
 
@@ -135,12 +144,14 @@ __device__ __forceinline__ Channel channel(const BnLayer &b, int ch) {
     return Channel{b.stats[ch], b.stats[b.C + ch], b.stats[2 * b.C + ch], b.stats[3 * b.C + ch]};
 }
 struct Place {
-    int n, i, left;
+    int n, k;
+    QuadAt at;
     int64_t plane;
 };
+template <bool WHOLE>
 __device__ __forceinline__ Place place(const BnLayer &b, int ch, int e) {
-    const int n = quotient(e, b.by_per), i = (e - n * (int)b.by_per.d) * 4;
-    return Place{n, i, b.HW - i, (int64_t)n * b.C + ch};
+    const int n = quotient(e, b.by_per), k = e - n * (int)b.by_per.d;
+    return Place{n, k, quad_at<WHOLE>(k, b.HW), (int64_t)n * b.C + ch};
 }
 // What a quad is made of; zeros where `live` is false.
 struct Quad {
@@ -148,16 +159,17 @@ struct Quad {
     float step;
     f4 da;
 };
-__device__ __forceinline__ Quad fetch(const BnLayer &b, const Place &at, int ch, bool live, const float *da, int64_t dsn, int64_t dsc) {
+template <bool WHOLE>
+__device__ __forceinline__ Quad fetch(const BnLayer &b, const Place &p, int ch, bool live, const float *da, int64_t dsn, int64_t dsc) {
     Quad q{0u, 0.f, f4{0.f, 0.f, 0.f, 0.f}};
     if (live) {
-        q.word = load_codes(b.q + at.plane * b.HW + at.i, at.left);
-        q.step = b.s[at.plane * b.G + at.i / kCkptGroup];
-        q.da = load4(da + (int64_t)at.n * dsn + (int64_t)ch * dsc + at.i, at.left);
+        q.word = load_codes<WHOLE>(b.q + p.plane * b.HW, p.at);
+        q.step = b.s[p.plane * b.G + p.k / (kCkptGroup / 4)];
+        q.da = load4<WHOLE>(da + (int64_t)p.n * dsn + (int64_t)ch * dsc, p.at);
     }
     return q;
 }
-// dz and x - mean (pixels that do not exist: dz is zero, as their da is)
+// dz and x - mean (pixels that are not the quad's own: dz is zero, as their da is)
 __device__ __forceinline__ void quad(const Quad &q, const Channel &c, f4 &dz, f4 &xm) {
     const f4 v = decode(q.word, q.step);
 #pragma unroll
@@ -167,29 +179,35 @@ __device__ __forceinline__ void quad(const Quad &q, const Channel &c, f4 &dz, f4
     }
 }
 
-__device__ __forceinline__ void put_quad(f4 r, int left, float *po, uint16_t *p16) {
-    if (p16) {  // dense bf16, nearest even: what the convolutions that read it would round it to
-        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-        const u16x4 h = __builtin_bit_cast(u16x4, __builtin_convertvector(r, bf16x4));
-        if (left >= 4) {
-            *reinterpret_cast<u16x4_any *>(p16) = h;
-        } else {
-            for (int j = 0; j < left; ++j) p16[j] = h[j];
-        }
-    } else {
-        store4(po, left, r);
+// r to a quad of the plane at `out` or, rounded to bf16, at `out16` (nearest even: what the convolutions that read it would
+// round it to)
+template <bool WHOLE>
+__device__ __forceinline__ void put_quad(f4 r, QuadAt q, float *out, uint16_t *out16) {
+    if (!out16) {
+        store4<WHOLE>(out, q, r);
+        return;
     }
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+    const u16x4 h = __builtin_bit_cast(u16x4, __builtin_convertvector(r, bf16x4));
+    if (WHOLE || (q.from == 0 && q.end == 4)) {
+        *reinterpret_cast<u16x4_any *>(out16 + q.i) = h;
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (q.owns(j)) out16[q.i + j] = h[j];
 }
 
 constexpr int kFly = 4;  // quads a thread requests before it uses the first
 
-// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads add in fp32 (at most a few
-// hundred terms each), everything above in double
+// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads (at most a few
+// hundred terms each) and wavefronts add in fp32, everything above in double
+template <bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, int share,
                                                              double2 *sums) {
     __shared__ double part[4][2];
-    const int ch = (int)blockIdx.y, total = b.N * (int)b.by_per.d;
-    const int first = (int)blockIdx.x * share, last = min(total, first + share);
+    const int ch = (int)blockIdx.x, total = b.N * (int)b.by_per.d;  // (channels first: neighbours in memory)
+    const int first = (int)blockIdx.y * share, last = min(total, first + share);
     const Channel c = channel(b, ch);
     float a0 = 0.f, a1 = 0.f;
     for (int e0 = first + (int)threadIdx.x; e0 < last; e0 += kFly * kThreads) {
@@ -197,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, co
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
             const int e = e0 + u * kThreads;
-            q[u] = fetch(b, place(b, ch, e < last ? e : e0), ch, e < last, da, dsn, dsc);
+            q[u] = fetch<WHOLE>(b, place<WHOLE>(b, ch, e < last ? e : e0), ch, e < last, da, dsn, dsc);
         }
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
@@ -210,11 +228,11 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, co
             }
         }
     }
-    const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
+    const float t0 = wave_total(a0), t1 = wave_total(a1);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = t0, part[threadIdx.x >> 6][1] = t1;
     __syncthreads();
     if (threadIdx.x == 0)
-        sums[(int64_t)ch * gridDim.x + blockIdx.x] =
+        sums[(int64_t)ch * gridDim.y + blockIdx.y] =
             make_double2((part[0][0] + part[1][0]) + (part[2][0] + part[3][0]), (part[0][1] + part[1][1]) + (part[2][1] + part[3][1]));
 }
 
@@ -239,7 +257,7 @@ __device__ __forceinline__ void put_sums(const Channel &c, double sum, double su
 }
 
 // The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
-template <bool SKIP>
+template <bool SKIP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc,
                                                             const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_chunks,
                                                             float *dgamma, float *dbeta, int accumulate, const float *skip, int64_t ksn,
@@ -258,34 +276,34 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
         const int e = e0 + u * kThreads;
-        const Place at = place(b, ch, e < total ? e : 0);
-        q[u] = fetch(b, at, ch, e < total, da, dsn, dsc);
-        if (SKIP && e < total) kv[u] = load4(skip + (int64_t)at.n * ksn + (int64_t)ch * ksc + at.i, at.left);
+        const Place p = place<WHOLE>(b, ch, e < total ? e : 0);
+        q[u] = fetch<WHOLE>(b, p, ch, e < total, da, dsn, dsc);
+        if (SKIP && e < total) kv[u] = load4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
     }
     // every wavefront adds the channel's partial sums for itself, in the same order
     const int lane = (int)threadIdx.x & 63;
-    double2 p = make_double2(0.0, 0.0);
-    if (lane < S) p = sums[(int64_t)ch * S + lane];
-    const double sum = wave_total(p.x), sum_xm = wave_total(p.y);
+    double2 part = make_double2(0.0, 0.0);
+    if (lane < S) part = sums[(int64_t)ch * S + lane];
+    const double sum = wave_total(part.x), sum_xm = wave_total(part.y);
     if (chunk == 0 && threadIdx.x == 0) put_sums(c, sum, sum_xm, dgamma, dbeta, ch, accumulate);
     const Coefs k = coefs(c, sum, sum_xm, inv_m);
 #pragma unroll
     for (int u = 0; u < kFly; ++u) {
         const int e = e0 + u * kThreads;
         if (e >= total) return;
-        const Place at = place(b, ch, e);
+        const Place p = place<WHOLE>(b, ch, e);
         f4 dz, xm;
         quad(q[u], c, dz, xm);
         f4 r = gradient(dz, xm, c, k);
         if (SKIP) r += kv[u];
-        put_quad(r, at.left, out + (int64_t)at.n * osn + (int64_t)ch * osc + at.i, out16 ? out16 + at.plane * b.HW + at.i : nullptr);
+        put_quad<WHOLE>(r, p.at, out + (int64_t)p.n * osn + (int64_t)ch * osc, out16 ? out16 + p.plane * b.HW : nullptr);
     }
 }
 
 // Both passes in one launch where a channel's quads fit the registers of one workgroup: codes and da are read once.
 constexpr int kFusedQuads = 8;
 
-template <int T, bool SKIP>
+template <int T, bool SKIP, bool WHOLE>
 __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, double inv_m,
                                                      float *dgamma, float *dbeta, int accumulate, const float *skip, int64_t ksn,
                                                      int64_t ksc, float *out, int64_t osn, int64_t osc, uint16_t *out16,
@@ -305,14 +323,14 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
 #pragma unroll
     for (int u = 0; u < kFusedQuads; ++u) {
         const int e = (int)threadIdx.x + u * T;
-        quad(fetch(b, place(b, ch, e < total ? e : 0), ch, e < total, da, dsn, dsc), c, dz[u], xm[u]);
+        quad(fetch<WHOLE>(b, place<WHOLE>(b, ch, e < total ? e : 0), ch, e < total, da, dsn, dsc), c, dz[u], xm[u]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             a0 += dz[u][j];
             a1 = fmaf(dz[u][j], xm[u][j], a1);
         }
     }
-    const double t0 = wave_total((double)a0), t1 = wave_total((double)a1);
+    const float t0 = wave_total(a0), t1 = wave_total(a1);
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6][0] = t0, part[threadIdx.x >> 6][1] = t1;
     __syncthreads();
     double sum = 0.0, sum_xm = 0.0;
@@ -324,10 +342,10 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
     for (int u = 0; u < kFusedQuads; ++u) {
         const int e = (int)threadIdx.x + u * T;
         if (e >= total) return;
-        const Place at = place(b, ch, e);
+        const Place p = place<WHOLE>(b, ch, e);
         f4 r = gradient(dz[u], xm[u], c, k);
-        if (SKIP) r += load4(skip + (int64_t)at.n * ksn + (int64_t)ch * ksc + at.i, at.left);
-        put_quad(r, at.left, out + (int64_t)at.n * osn + (int64_t)ch * osc + at.i, out16 ? out16 + at.plane * b.HW + at.i : nullptr);
+        if (SKIP) r += load4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
+        put_quad<WHOLE>(r, p.at, out + (int64_t)p.n * osn + (int64_t)ch * osc, out16 ? out16 + p.plane * b.HW : nullptr);
     }
 }
 
@@ -352,10 +370,9 @@ void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k) {
     while (tshift < 4 && (4 << tshift) < hw) ++tshift;
     const int pairs = (g.n + 1) / 2;
     const dim3 grid(blocks_for((int64_t)c * G, kThreads >> tshift), (unsigned)(pairs < 65535 ? pairs : 65535));
-    if (stats)
-        cx.run(ckpt_save_k<true>, grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
-    else
-        cx.run(ckpt_save_k<false>, grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
+    const bool whole = hw % 4 == 0;
+    cx.run(stats ? (whole ? ckpt_save_k<true, true> : ckpt_save_k<true, false>) : (whole ? ckpt_save_k<false, true> : ckpt_save_k<false, false>),
+           grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
 }
 
 void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out) {
@@ -363,7 +380,7 @@ void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out) {
     const double planes = (double)g.n * c;
     if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
     const dim3 grid(blocks_for((int64_t)c * per, kThreads), (unsigned)(g.n < 65535 ? g.n : 65535));
-    cx.run(ckpt_load_k, grid, dim3(kThreads), 0, k.q, k.s, g.n, c, hw, G, fast_div(per), out.p, out.sn, out.sc);
+    cx.run(hw % 4 == 0 ? ckpt_load_k<true> : ckpt_load_k<false>, grid, dim3(kThreads), 0, k.q, k.s, g.n, c, hw, G, fast_div(per), out.p, out.sn, out.sc);
 }
 
 size_t ckpt_bn_scratch_floats(int c, const Geo &g) { return (size_t)c * ckpt_bn_splits(c, g) * 4; }
@@ -384,12 +401,12 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
     const View kv = skip ? *skip : View{nullptr, 0, 0};
     const int acc = accumulate ? 1 : 0;
     const double out_bytes = out16 ? 2.0 : skip ? 8.0 : 4.0;
-    const bool wide = total > kFusedQuads * kThreads;
+    const bool wide = total > kFusedQuads * kThreads, whole = hw % 4 == 0;
     if (total <= kFusedQuads * 1024 && !(wide && (red.blocks > 0 || c < 256))) {
         if (!cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) return;
         const dim3 grid((unsigned)(c + red.blocks));
 #define RVN_FUSED(T, K)                                                                                                          \
-    cx.run(ckpt_bn_fused_k<T, K>, grid, dim3(T), 0, b, da.p, da.sn, da.sc, inv_m, dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p, \
+    cx.run(whole ? ckpt_bn_fused_k<T, K, true> : ckpt_bn_fused_k<T, K, false>, grid, dim3(T), 0, b, da.p, da.sn, da.sc, inv_m, dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p, \
            out.sn, out.sc, out16, red)
         if (wide && skip) RVN_FUSED(1024, true);
         else if (wide) RVN_FUSED(1024, false);
@@ -401,16 +418,14 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
     const int S = ckpt_bn_splits(c, g), share = (total + S - 1) / S;
     double2 *sums = reinterpret_cast<double2 *>(scratch);
     if (cx.launch(K_BN_BWD_REDUCE, 5.0 * elems))
-        cx.run(ckpt_bn_reduce_k, dim3((unsigned)S, (unsigned)c), dim3(kThreads), 0, b, da.p, da.sn, da.sc, share, sums);
+        cx.run(whole ? ckpt_bn_reduce_k<true> : ckpt_bn_reduce_k<false>, dim3((unsigned)c, (unsigned)S), dim3(kThreads), 0, b, da.p, da.sn, da.sc, share, sums);
     if (cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) {
         const int chunks = (total + kFly * kThreads - 1) / (kFly * kThreads);
         const dim3 grid((unsigned)(chunks * c + red.blocks));
-        if (skip)
-            cx.run(ckpt_bn_apply_k<true>, grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta,
-                   acc, kv.p, kv.sn, kv.sc, out.p, out.sn, out.sc, out16, red);
-        else
-            cx.run(ckpt_bn_apply_k<false>, grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta,
-                   acc, kv.p, kv.sn, kv.sc, out.p, out.sn, out.sc, out16, red);
+        cx.run(skip ? (whole ? ckpt_bn_apply_k<true, true> : ckpt_bn_apply_k<true, false>)
+                    : (whole ? ckpt_bn_apply_k<false, true> : ckpt_bn_apply_k<false, false>),
+               grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p,
+               out.sn, out.sc, out16, red);
     }
 }
 

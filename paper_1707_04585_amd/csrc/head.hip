@@ -9,6 +9,8 @@
 // and one pass reads x and writes dx = scale * ((z > 0 ? g_n : 0) - mean(dz) - xhat * mean(dz * xhat)).
 // x is bound by memory: 4 bytes an element forward, 8 backward.  The products are small (n up to a few hundred): bound
 // by the latency of their loads, hence one 16x16 tile per workgroup and its reduction split over the wavefronts.
+#include <algorithm>
+
 #include "fast_div.h"
 #include "kernels.h"
 #include "quads.h"
@@ -19,19 +21,16 @@ namespace {
 
 // ---- pooling ---------------------------------------------------------------------------------------------------
 
-constexpr int kHeld = 8;  // quads a lane keeps in registers
-
 // How a channel's planes fall to wavefronts: 2^tshift lanes share a plane of `per` quads, J of them each; a wavefront takes
 // 64 >> tshift planes at a time, `steps` times.
 struct Planes {
     int N, C, HW, per, tshift, J, steps;
 };
 
-// The sum over the workgroup of a value of each thread, in every thread.
+// The sum over the workgroup of a value of each thread, in every thread: wavefronts in fp32, their sums in double.
 template <int TH>
 __device__ __forceinline__ double block_total(float v, double *lds) {
-    const double t = wave_total((double)v);
-    __syncthreads();
+    const float t = wave_total(v);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = t;
     __syncthreads();
     double s = 0.0;
@@ -40,52 +39,70 @@ __device__ __forceinline__ double block_total(float v, double *lds) {
     return s;
 }
 
-// HELD: steps * J <= kHeld, and the channel stays in registers; otherwise it is read three times (the second and third
-// mostly from the caches).
-template <int TH, bool HELD>
+// HELD > 0: the channel stays in registers, steps * J <= HELD quads of it in each lane; otherwise it is read three times (the
+// second and third mostly from the caches).
+template <int TH, int HELD, bool WHOLE>
 __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, int64_t sn, int64_t sc, const Planes g, float eps,
                                                   const float *__restrict__ gamma, const float *__restrict__ beta,
                                                   float *__restrict__ stats, float *__restrict__ pooled, float *__restrict__ count,
                                                   float *__restrict__ xhat) {
-    __shared__ double lds[TH / 64];
+    __shared__ float lds[TH / 64][3];
     const int ch = (int)blockIdx.x, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
     const int T = 1 << g.tshift, sub = lane & (T - 1), planes = 64 >> g.tshift;
     const float *base = x + (int64_t)ch * sc;
-    f4 held[kHeld];
-    // calls visit(value, plane, pixels left) for every item of this lane, in order; a plane's items follow each other
+    f4 held[HELD > 0 ? HELD : 1];
+    // calls visit(value, plane, its quad, whether it exists, whether it is the plane's last) for every item of this lane, in
+    // order; a plane's items follow each other
     auto each = [&](bool first, auto visit) {
         int step = 0, j = 0;
         auto item = [&](int k) {
             const int n = (step * (TH / 64) + wave) * planes + (lane >> g.tshift), quad = j * T + sub;
-            const int left = n < g.N && quad < g.per ? g.HW - quad * 4 : 0;
+            const bool live = n < g.N && quad < g.per;
+            const QuadAt at = quad_at<WHOLE>(quad, g.HW);
             f4 v = {0.f, 0.f, 0.f, 0.f};
-            if (HELD && !first) v = held[k];
-            else if (left > 0) v = load4(base + (int64_t)n * sn + quad * 4, left);
-            if (HELD && first) held[k] = v;
-            visit(v, n, left, j == g.J - 1);
+            if (HELD > 0 && !first) v = held[k];
+            else if (live) v = load4<WHOLE>(base + (int64_t)n * sn, at);
+            if (HELD > 0 && first) held[k] = v;
+            visit(v, n, at, live, j == g.J - 1);
             if (++j == g.J) j = 0, ++step;
         };
-        if constexpr (HELD) {
+        if constexpr (HELD > 0) {
 #pragma unroll
-            for (int k = 0; k < kHeld; ++k)
+            for (int k = 0; k < HELD; ++k)
                 if (step < g.steps) item(k);
         } else {
             while (step < g.steps) item(0);
         }
     };
-    float a = 0.f;
-    each(true, [&](f4 v, int, int, bool) { a += (v.x + v.y) + (v.z + v.w); });
-    const double m = (double)g.N * g.HW;
-    const float mean = (float)(block_total<TH>(a, lds) / m);
-    a = 0.f;
-    each(false, [&](f4 v, int, int left, bool) {
+    // mean and squared deviations of every wavefront's pixels, joined over the workgroup in double
+    float sum = 0.f, pos = 0.f, hat = 0.f;
+    each(true, [&](f4 v, int, QuadAt at, bool live, bool) {
+        sum += (v.x + v.y) + (v.z + v.w);
+        if (live) pos += WHOLE ? 4.f : (float)(at.end - at.from);
+    });
+    const float here = wave_total(pos), wave_mean = here > 0.f ? wave_total(sum) / here : 0.f;
+    sum = 0.f;
+    each(false, [&](f4 v, int, QuadAt at, bool live, bool) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float d = e < left ? v[e] - mean : 0.f;
-            a = fmaf(d, d, a);
+            const float d = live && at.owns(e) ? v[e] - wave_mean : 0.f;
+            sum = fmaf(d, d, sum);
         }
     });
-    const float rstd = (float)(1.0 / sqrt(block_total<TH>(a, lds) / m + (double)eps));
+    sum = wave_total(sum);
+    if (lane == 0) lds[wave][0] = here, lds[wave][1] = wave_mean, lds[wave][2] = sum;
+    __syncthreads();
+    const double m = (double)g.N * g.HW;
+    double total = 0.0, m2 = 0.0;
+#pragma unroll 4
+    for (int w = 0; w < TH / 64; ++w) total += (double)lds[w][0] * lds[w][1];
+    const double mean_d = total / m;
+#pragma unroll 4
+    for (int w = 0; w < TH / 64; ++w) {
+        const double d = lds[w][1] - mean_d;
+        m2 += lds[w][2] + lds[w][0] * d * d;
+    }
+    const float mean = (float)mean_d, rstd = 1.f / sqrtf((float)(m2 / m) + eps);
     const float scale = gamma[ch] * rstd, shift = fmaf(-mean, scale, beta[ch]);
     if (threadIdx.x == 0) {
         stats[ch] = mean;
@@ -94,25 +111,23 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
         stats[3 * g.C + ch] = shift;
     }
     const float inv_hw = 1.f / (float)g.HW;
-    float sum = 0.f, pos = 0.f, hat = 0.f;
-    each(false, [&](f4 v, int n, int left, bool last) {
+    sum = pos = 0.f;
+    each(false, [&](f4 v, int n, QuadAt at, bool live, bool last) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float z = fmaf(v[e], scale, shift);
-            if (e < left && z > 0.f) {
+            if (live && at.owns(e) && z > 0.f) {
                 sum += z;
                 pos += 1.f;
                 hat += (v[e] - mean) * rstd;
             }
         }
         if (!last) return;
-        for (int o = T >> 1; o > 0; o >>= 1) {
-            sum += __shfl_xor(sum, o, 64);
-            pos += __shfl_xor(pos, o, 64);
-            hat += __shfl_xor(hat, o, 64);
-        }
+        sum = team_total(sum, g.tshift);
+        pos = team_total(pos, g.tshift);
+        hat = team_total(hat, g.tshift);
         if (sub == 0 && n < g.N) {
-            pooled[(int64_t)n * g.C + ch] = sum * inv_hw;
+            pooled[(int64_t)ch * g.N + n] = sum * inv_hw;
             count[(int64_t)ch * g.N + n] = pos;
             xhat[(int64_t)ch * g.N + n] = hat;
         }
@@ -123,12 +138,13 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
 // dx of a share of a channel's quads; every workgroup forms the channel's two sums for itself.
 constexpr int kPoolThreads = 256;
 
+template <bool WHOLE>
 __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__restrict__ x, int64_t sn, int64_t sc, int N, int C, int HW,
                                                                 FastDiv by_per, int share, const float *__restrict__ stats,
                                                                 const float *__restrict__ count, const float *__restrict__ xhat,
                                                                 const float *__restrict__ d_pooled, float *dgamma, float *dbeta,
                                                                 int accumulate, float *__restrict__ dx, int64_t osn, int64_t osc) {
-    __shared__ double lds[kPoolThreads / 64];
+    __shared__ double lds[2][kPoolThreads / 64];
     const int ch = (int)blockIdx.y, per = (int)by_per.d, total = N * per;
     const float mean = stats[ch], rstd = stats[C + ch], scale = stats[2 * C + ch], shift = stats[3 * C + ch];
     const float inv_hw = 1.f / (float)HW;
@@ -139,7 +155,7 @@ __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__r
         a0 = fmaf(gn, cnt[n], a0);
         a1 = fmaf(gn, hat[n], a1);
     }
-    const double sb = block_total<kPoolThreads>(a0, lds), sg = block_total<kPoolThreads>(a1, lds);
+    const double sb = block_total<kPoolThreads>(a0, lds[0]), sg = block_total<kPoolThreads>(a1, lds[1]);
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         dbeta[ch] = (accumulate ? dbeta[ch] : 0.f) + (float)sb;
         dgamma[ch] = (accumulate ? dgamma[ch] : 0.f) + (float)sg;
@@ -148,8 +164,9 @@ __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__r
     const float c1 = (float)(sb * inv_m), c2 = (float)(sg * inv_m);
     const int last = min(total, ((int)blockIdx.x + 1) * share);
     for (int e = (int)blockIdx.x * share + (int)threadIdx.x; e < last; e += kPoolThreads) {
-        const int n = quotient(e, by_per), i = (e - n * per) * 4, left = HW - i;
-        const f4 v = load4(x + (int64_t)n * sn + (int64_t)ch * sc + i, left);
+        const int n = quotient(e, by_per);
+        const QuadAt at = quad_at<WHOLE>(e - n * per, HW);
+        const f4 v = load4<WHOLE>(x + (int64_t)n * sn + (int64_t)ch * sc, at);
         const float gn = g[n] * inv_hw;
         f4 r;
 #pragma unroll
@@ -157,118 +174,200 @@ __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__r
             const float dz = fmaf(v[j], scale, shift) > 0.f ? gn : 0.f;
             r[j] = scale * ((dz - c1) - ((v[j] - mean) * rstd) * c2);
         }
-        store4(dx + (int64_t)n * osn + (int64_t)ch * osc + i, left, r);
+        store4<WHOLE>(dx + (int64_t)n * osn + (int64_t)ch * osc, at, r);
     }
 }
 
 // ---- products on v_mfma_f32_16x16x4_f32 -----------------------------------------------------------------------
 // Lane l holds row (or column) l % 16 of an operand at reduction index l / 16 and, of the result, column l % 16 of rows
-// (l / 16) * 4 .. + 3.  Four instructions take 16 reduction indices: the lanes of group l / 16 the four from (l / 16) * 4.
+// (l / 16) * 4 .. + 3.  Which reduction index stands at which place is free as long as both operands agree.
 
-// Operand whose reduction index runs along memory: row `r` at p + r * ld; what lies at or behind k1 reads as zero.
-__device__ __forceinline__ f4 along(const float *p, int64_t ld, int r, int k, int k1) {
-    if (k >= k1) return f4{0.f, 0.f, 0.f, 0.f};
-    return load4(p + (int64_t)r * ld + k, k1 - k);
-}
-// Operand whose reduction index runs across it: index k at p + k * ld + r.
-__device__ __forceinline__ f4 across(const float *p, int64_t ld, int r, int k, int k1) {
-    f4 v;
+// An operand of 16 rows (or columns): row r at p + r * ld where its reduction index runs along memory, else index k at
+// p + k * ld; rows beyond `count` are taken for the last one.
+template <bool ALONG>
+struct Operand {
+    const float *p;
+    int64_t ld;
+    // first: the first of the 16 rows of the matrix
+    __device__ __forceinline__ Operand(const float *m, int64_t l, int first, int count) : ld(l) {
+        const int lane = (int)threadIdx.x & 63;
+        p = ALONG ? m + (int64_t)min(first + (lane >> 2), count - 1) * l + (lane & 3) * 4 : m + min(first + (lane & 15), count - 1);
+    }
+    // What the lane reads for reduction indices k .. k + 15.  Across memory that is its own four values, with 16 lanes side by
+    // side; along memory, where the rows are far apart, four lanes read 64 bytes of a row together (lane by lane in the order
+    // of the rows each would be an access of its own: 62 cycles an instruction).  FULL: k + 16 <= k1; else what lies at or
+    // behind k1 reads as zero.
+    template <bool FULL>
+    __device__ __forceinline__ f4 fetch(int k, int k1) const {
+        const int lane = (int)threadIdx.x & 63;
+        f4 v = {0.f, 0.f, 0.f, 0.f};
+        if (ALONG) {
+            if (FULL) return *reinterpret_cast<const f4_any *>(p + k);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = k + e < k1 ? p[(int64_t)(k + e) * ld + r] : 0.f;
-    return v;
-}
+            for (int e = 0; e < 4; ++e) v[e] = k + (lane & 3) * 4 + e < k1 ? p[k + e] : 0.f;
+        } else {
+            const int mine = k + (lane >> 4) * 4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = FULL || mine + e < k1 ? p[(mine + e) * ld] : 0.f;
+        }
+        return v;
+    }
+    // The lane's own four values from what was fetched; lds: kTurn floats of the wavefront's own.
+    static constexpr int kPitch = 20;
+    static __device__ __forceinline__ f4 own(f4 v, float *lds) {
+        if (!ALONG) return v;
+        const int lane = (int)threadIdx.x & 63;
+        *reinterpret_cast<f4 *>(lds + (lane >> 2) * kPitch + (lane & 3) * 4) = v;
+        __builtin_amdgcn_wave_barrier();
+        v = *reinterpret_cast<const f4 *>(lds + (lane & 15) * kPitch + (lane >> 4) * 4);
+        __builtin_amdgcn_wave_barrier();
+        return v;
+    }
+};
+constexpr int kTurn = 16 * Operand<true>::kPitch;
 __device__ __forceinline__ f4 multiply(f4 a, f4 b, f4 c) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[e], b[e], c, 0, 0, 0);
     return c;
 }
 
-// The 16x16 tile at (m0, n0) of the product of an M x K and a K x N operand, its K split over the wavefronts of the
-// workgroup and added in their order; put(m, n, value) stores an element that exists.
-template <bool B_ALONG, typename Put>
-__device__ __forceinline__ void tile(const float *a, int64_t lda, int M, int m0, const float *b, int64_t ldb, int N, int n0, int K,
-                                     float *lds, Put put) {
-    const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, waves = (int)blockDim.x >> 6;
-    const int steps = (K + 15) / 16, each = (steps + waves - 1) / waves;
-    const int k0 = wave * each * 16, k1 = min(K, k0 + each * 16);
-    const int r = min(m0 + (lane & 15), M - 1), c = min(n0 + (lane & 15), N - 1);  // (beyond the edge: computed, not stored)
-    f4 sum = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < each; ++s) {
-        const int k = k0 + s * 16 + (lane >> 4) * 4;
-        const f4 va = along(a, lda, r, k, k1);
-        const f4 vb = B_ALONG ? along(b, ldb, c, k, k1) : across(b, ldb, c, k, k1);
-        sum = multiply(va, vb, sum);
-    }
+// sum[t] += the product over reduction indices k0 .. k1 - 1 of A and B[t]; the lanes' own sums of A's values are added to *rows.
+// The operands of kAhead steps of 16 are requested together.
+template <int kAhead, bool A_ALONG, bool B_ALONG, int NT>
+__device__ __forceinline__ void accumulate_product(const Operand<A_ALONG> &a, const Operand<B_ALONG> (&b)[NT], int k0, int k1, float *lds,
+                                                   f4 (&sum)[NT], float *rows) {
+    auto add = [&](f4 va, const f4 (&vb)[NT]) {
+        va = a.own(va, lds);
+        *rows += (va.x + va.y) + (va.z + va.w);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) lds[wave * 256 + ((lane >> 4) * 4 + e) * 16 + (lane & 15)] = sum[e];
-    __syncthreads();
-    for (int o = (int)threadIdx.x; o < 256; o += (int)blockDim.x) {
-        float t = 0.f;
-        for (int w = 0; w < waves; ++w) t += lds[w * 256 + o];
-        const int m = m0 + o / 16, n = n0 + o % 16;
-        if (m < M && n < N) put(m, n, t);
+        for (int t = 0; t < NT; ++t) sum[t] = multiply(va, b[t].own(vb[t], lds + kTurn), sum[t]);
+    };
+    int k = k0;
+    for (; k + 16 * kAhead <= k1; k += 16 * kAhead) {
+        f4 va[kAhead], vb[kAhead][NT];
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) {
+            va[s] = a.template fetch<true>(k + 16 * s, k1);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) vb[s][t] = b[t].template fetch<true>(k + 16 * s, k1);
+        }
+        __builtin_amdgcn_sched_barrier(0);  // (left alone the compiler moves the loads to their uses, two or three in flight)
+#pragma unroll
+        for (int s = 0; s < kAhead; ++s) add(va[s], vb[s]);
+    }
+    for (; k < k1; k += 16) {
+        const bool full = k + 16 <= k1;
+        const f4 va = full ? a.template fetch<true>(k, k1) : a.template fetch<false>(k, k1);
+        f4 vb[NT];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) vb[t] = full ? b[t].template fetch<true>(k, k1) : b[t].template fetch<false>(k, k1);
+        add(va, vb);
     }
 }
 
-constexpr int kMostWaves = 16;
+template <int WAVES>
+struct TileLds {
+    union {
+        float turn[WAVES][2 * kTurn];  // while a wavefront adds its products
+        float part[WAVES * 256];       // afterwards
+    };
+    float rows[WAVES * 16];
+};
 
-__global__ __launch_bounds__(kMostWaves * 64) void head_linear_k(const float *__restrict__ pooled, int n, int c, int classes,
+// The 16 x WIDE tile at (m0, n0) of the product of an M x K and a K x N operand, its K split over the wavefronts of the
+// workgroup and added in their order; put(m, n, value) stores an element that exists, put_rows(m, value) the sum of row m of A.
+template <int kAhead, bool A_ALONG, bool B_ALONG, int WIDE = 16, typename Lds, typename Put, typename PutRows>
+__device__ __forceinline__ void tile(const float *a, int64_t lda, int M, int m0, const float *b, int64_t ldb, int N, int n0, int K,
+                                     Lds &lds, Put put, PutRows put_rows) {
+    const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, waves = (int)blockDim.x >> 6;
+    const int each = ((K + 15) / 16 + waves - 1) / waves * 16, k0 = wave * each, k1 = min(K, k0 + each);
+    const Operand<A_ALONG> oa(a, lda, m0, M);                                   // (rows and columns beyond the edge are computed,
+    const Operand<B_ALONG> ob[1] = {Operand<B_ALONG>(b, ldb, n0, min(N, n0 + WIDE))};  //  not stored)
+    f4 sum[1] = {{0.f, 0.f, 0.f, 0.f}};
+    float rows = 0.f;
+    accumulate_product<kAhead>(oa, ob, k0, k1, lds.turn[wave], sum, &rows);
+    __syncthreads();
+    rows += __shfl_xor(rows, 16, 64);
+    rows += __shfl_xor(rows, 32, 64);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) lds.part[wave * 256 + ((lane >> 4) * 4 + e) * 16 + (lane & 15)] = sum[0][e];
+    if (lane < 16) lds.rows[wave * 16 + lane] = rows;
+    __syncthreads();
+    for (int o = (int)threadIdx.x; o < 256 + 16; o += (int)blockDim.x) {
+        const bool row = o >= 256;
+        float t = 0.f;
+#pragma unroll 4
+        for (int w = 0; w < waves; ++w) t += row ? lds.rows[w * 16 + o - 256] : lds.part[w * 256 + o];
+        const int m = m0 + (row ? o - 256 : o / 16), n = n0 + o % 16;
+        if (m >= M) continue;
+        if (row) put_rows(m, t);
+        else if (n < N && o % 16 < WIDE) put(m, n, t);
+    }
+}
+
+constexpr int kForwardWaves = 16, kBackwardWaves = 8;  // the most of a workgroup
+
+template <int WIDE>
+__global__ __launch_bounds__(kForwardWaves * 64) void head_linear_k(const float *__restrict__ pooled, int n, int c, int classes,
                                                                  const float *__restrict__ w, const float *__restrict__ b,
                                                                  float *__restrict__ logits, int64_t ld) {
-    __shared__ float lds[kMostWaves * 256];
-    tile<true>(pooled, c, n, (int)blockIdx.y * 16, w, c, classes, (int)blockIdx.x * 16, c, lds,
-               [&](int i, int k, float v) { logits[(int64_t)i * ld + k] = v + b[k]; });
+    __shared__ TileLds<kForwardWaves> lds;
+    tile<8, false, true, WIDE>(pooled, n, n, (int)blockIdx.y * 16, w, c, classes, (int)blockIdx.x * WIDE, c, lds,
+                     [&](int i, int k, float v) { logits[(int64_t)i * ld + k] = v + b[k]; }, [](int, float) {});
 }
 
-// The first `data_blocks` workgroups: d_pooled as [c][n], a tile each.  The others: the weights' gradient, a strip of 16
-// classes by 64 channels per wavefront, and in the strips of the first channels the bias's.
-__global__ __launch_bounds__(kMostWaves * 64) void head_linear_bwd_k(const float *__restrict__ dl, int64_t ld, const float *__restrict__ pooled,
+// The first `data_blocks` workgroups: d_pooled as [c][n], a tile each.  The others: the weights' gradient and, where the
+// channels begin, the bias's -- STRIPS: 16 classes by 64 channels per wavefront, which reads the 16 classes' derivatives once
+// for four tiles; else, where that leaves most of the chip idle, a tile per workgroup with the images split over its wavefronts.
+template <bool STRIPS>
+__global__ __launch_bounds__(kBackwardWaves * 64, 4) void head_linear_bwd_k(const float *__restrict__ dl, int64_t ld, const float *__restrict__ pooled,
                                                                      int n, int c, int classes, const float *__restrict__ w,
                                                                      float *__restrict__ d_pooled, float *dw, float *db, int accumulate,
                                                                      int data_blocks) {
-    __shared__ float lds[kMostWaves * 256];
+    __shared__ TileLds<kBackwardWaves> lds;
+    const int tiles_c = (c + 15) / 16;
     if ((int)blockIdx.x < data_blocks) {
-        const int tiles_c = (c + 15) / 16, tm = (int)blockIdx.x / tiles_c, tc = (int)blockIdx.x - tm * tiles_c;
-        tile<false>(dl, ld, n, tm * 16, w, c, c, tc * 16, classes, lds, [&](int i, int ch, float v) { d_pooled[(int64_t)ch * n + i] = v; });
+        const int tm = (int)blockIdx.x / tiles_c, tc = (int)blockIdx.x - tm * tiles_c;
+        tile<4, true, false>(dl, ld, n, tm * 16, w, c, c, tc * 16, classes, lds,
+                          [&](int i, int ch, float v) { d_pooled[(int64_t)ch * n + i] = v; }, [](int, float) {});
         return;
     }
-    const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, waves = (int)blockDim.x >> 6;
-    const int strips_c = (c + 63) / 64, strips = strips_c * ((classes + 15) / 16);
-    const int strip = ((int)blockIdx.x - data_blocks) * waves + wave;
-    if (strip >= strips) return;
-    const int sk = strip / strips_c, c0 = (strip - sk * strips_c) * 64, k0 = sk * 16;
-    const int r = min(k0 + (lane & 15), classes - 1);
-    f4 sum[4] = {};
-    float bias = 0.f;
-    for (int i = (lane >> 4) * 4, s = 0; s < (n + 15) / 16; ++s, i += 16) {
-        const f4 va = across(dl, ld, r, i, n);
-        bias += (va.x + va.y) + (va.z + va.w);
+    const int block = (int)blockIdx.x - data_blocks;
+    auto put_bias = [&](int k, float v) { db[k] = (accumulate ? db[k] : 0.f) + v; };
+    auto put_weight = [&](int k, int ch, float v) {
+        float *to = dw + (int64_t)k * c + ch;
+        *to = (accumulate ? *to : 0.f) + v;
+    };
+    if constexpr (!STRIPS) {
+        const int tk = block / tiles_c, tc = block - tk * tiles_c;
+        tile<4, false, true>(dl, ld, classes, tk * 16, pooled, n, c, tc * 16, n, lds, put_weight, [&](int k, float v) {
+            if (tc == 0) put_bias(k, v);
+        });
+    } else {
+        const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, waves = (int)blockDim.x >> 6;
+        const int strips_c = (c + 63) / 64, strip = block * waves + wave;
+        if (strip >= strips_c * ((classes + 15) / 16)) return;
+        const int sk = strip / strips_c, c0 = (strip - sk * strips_c) * 64, k0 = sk * 16;
+        const Operand<false> oa(dl, ld, k0, classes);
+        const Operand<true> ob[4] = {{pooled, n, c0, c}, {pooled, n, c0 + 16, c}, {pooled, n, c0 + 32, c}, {pooled, n, c0 + 48, c}};
+        f4 sum[4] = {};
+        float bias = 0.f;
+        accumulate_product<1>(oa, ob, 0, n, lds.turn[wave], sum, &bias);
 #pragma unroll
-        for (int t = 0; t < 4; ++t) sum[t] = multiply(va, across(pooled, c, min(c0 + t * 16 + (lane & 15), c - 1), i, n), sum[t]);
-    }
+        for (int t = 0; t < 4; ++t)
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        const int ch = c0 + t * 16 + (lane & 15);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int k = k0 + (lane >> 4) * 4 + e;
-            if (k >= classes || ch >= c) continue;
-            float *to = dw + (int64_t)k * c + ch;
-            *to = (accumulate ? *to : 0.f) + sum[t][e];
-        }
-    }
-    if (c0 == 0) {
+            for (int e = 0; e < 4; ++e) {
+                const int k = k0 + (lane >> 4) * 4 + e, ch = c0 + t * 16 + (lane & 15);
+                if (k < classes && ch < c) put_weight(k, ch, sum[t][e]);
+            }
         bias += __shfl_xor(bias, 16, 64);
         bias += __shfl_xor(bias, 32, 64);
-        if (lane < 16 && k0 + lane < classes) db[k0 + lane] = (accumulate ? db[k0 + lane] : 0.f) + bias;
+        if (c0 == 0 && lane < 16 && k0 + lane < classes) put_bias(k0 + lane, bias);
     }
 }
 
 // Wavefronts that share a reduction of length K: at least two steps of 16 each.
-int waves_for(int K) {
-    const int w = (K + 31) / 32;
-    return w < 1 ? 1 : w < kMostWaves ? w : kMostWaves;
-}
+int waves_for(int K, int most) { return std::max(1, std::min(most, (K + 31) / 32)); }
 
 }  // namespace
 
@@ -279,30 +378,40 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
     p.J = (p.per + (1 << p.tshift) - 1) >> p.tshift;
     const int at_once = 64 >> p.tshift;
     auto steps = [&](int waves) { return (g.n + waves * at_once - 1) / (waves * at_once); };
-    const bool small = steps(4) * p.J <= kHeld;
-    p.steps = steps(small ? 4 : 16);
+    // The fixed work of a wavefront (sums over lanes, statistics) outweighs a few quads a lane: as few wavefronts a channel as
+    // keep its quads in registers, eight a lane, and give every SIMD two of them.
+    constexpr int kWavesWanted = 8192;
+    int waves = 1;
+    while (waves < 16 && ((int64_t)c * waves < kWavesWanted || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
+    p.steps = steps(waves);
+    const bool held = (int64_t)p.steps * p.J <= 8, whole = g.hw() % 4 == 0;
 #define RVN_POOL(TH, HELD)                                                                                                     \
-    cx.run(head_pool_k<TH, HELD>, dim3((unsigned)c), dim3(TH), 0, x.p, x.sn, x.sc, p, eps, gamma, beta, s.stats, s.pooled, s.count, \
-           s.xhat)
-    if (small) RVN_POOL(256, true);
-    else if ((int64_t)p.steps * p.J <= kHeld) RVN_POOL(1024, true);
-    else RVN_POOL(1024, false);
+    cx.run(whole ? head_pool_k<TH, HELD, true> : head_pool_k<TH, HELD, false>, dim3((unsigned)c), dim3(TH), 0, x.p, x.sn, x.sc, p, eps, \
+           gamma, beta, s.stats, s.pooled, s.count, s.xhat)
+    if (!held) RVN_POOL(1024, 0);
+    else if (waves == 1) RVN_POOL(64, 8);
+    else if (waves == 4) RVN_POOL(256, 8);
+    else RVN_POOL(1024, 8);
 #undef RVN_POOL
 }
 
 void head_linear(Ctx &cx, const float *pooled, int n, int c, int classes, const float *w, const float *b, float *logits, int64_t ld) {
     if (!cx.launch(K_HEAD, 4.0 * ((double)n * c + (double)classes * c + (double)n * classes), 2.0 * n * (double)c * classes)) return;
-    cx.run(head_linear_k, dim3((unsigned)((classes + 15) / 16), (unsigned)((n + 15) / 16)), dim3((unsigned)(64 * waves_for(c))), 0, pooled, n,
-           c, classes, w, b, logits, ld);
+    const int rows = (n + 15) / 16, wide = (classes + 15) / 16 * rows >= 256 ? 16 : 8;
+    cx.run(wide == 16 ? head_linear_k<16> : head_linear_k<8>, dim3((unsigned)((classes + wide - 1) / wide), (unsigned)rows),
+           dim3((unsigned)(64 * waves_for(c, kForwardWaves))), 0, pooled, n, c, classes, w, b, logits, ld);
 }
 
 void head_linear_bwd(Ctx &cx, const float *dl, int64_t ld, const float *pooled, int n, int c, int classes, const float *w,
                      float *d_pooled, float *dw, float *db, bool accumulate) {
     if (!cx.launch(K_HEAD, 4.0 * (2.0 * n * c + 2.0 * classes * (double)c + (double)n * classes), 4.0 * n * (double)c * classes)) return;
-    const int waves = waves_for(classes), data_blocks = ((c + 15) / 16) * ((n + 15) / 16);
-    const int strips = ((c + 63) / 64) * ((classes + 15) / 16);
-    cx.run(head_linear_bwd_k, dim3((unsigned)(data_blocks + (strips + waves - 1) / waves)), dim3((unsigned)(64 * waves)), 0, dl, ld, pooled, n, c,
-           classes, w, d_pooled, dw, db, accumulate ? 1 : 0, data_blocks);
+    const int tiles_c = (c + 15) / 16, tiles_k = (classes + 15) / 16, data_blocks = tiles_c * ((n + 15) / 16);
+    const int strips = ((c + 63) / 64) * tiles_k;
+    const bool in_strips = strips >= 1024;  // a wavefront for every SIMD
+    const int waves = waves_for(in_strips ? classes : std::max(classes, n), kBackwardWaves);
+    cx.run(in_strips ? head_linear_bwd_k<true> : head_linear_bwd_k<false>,
+           dim3((unsigned)(data_blocks + (in_strips ? (strips + waves - 1) / waves : tiles_c * tiles_k))), dim3((unsigned)(64 * waves)), 0, dl, ld,
+           pooled, n, c, classes, w, d_pooled, dw, db, accumulate ? 1 : 0, data_blocks);
 }
 
 void head_pool_bwd(Ctx &cx, View x, int c, Geo g, HeadSaved s, const float *d_pooled, float *dgamma, float *dbeta, bool accumulate,
@@ -314,7 +423,7 @@ void head_pool_bwd(Ctx &cx, View x, int c, Geo g, HeadSaved s, const float *d_po
     const int most = (total + 4 * kPoolThreads - 1) / (4 * kPoolThreads);
     splits = splits < most ? splits : most;
     const int share = (total + splits - 1) / splits;
-    cx.run(head_pool_bwd_k, dim3((unsigned)splits, (unsigned)c), dim3(kPoolThreads), 0, x.p, x.sn, x.sc, g.n, c, g.hw(), fast_div(per), share,
+    cx.run(g.hw() % 4 == 0 ? head_pool_bwd_k<true> : head_pool_bwd_k<false>, dim3((unsigned)splits, (unsigned)c), dim3(kPoolThreads), 0, x.p, x.sn, x.sc, g.n, c, g.hw(), fast_div(per), share,
            s.stats, s.count, s.xhat, d_pooled, dgamma, dbeta, accumulate ? 1 : 0, dx.p, dx.sn, dx.sc);
 }
 

@@ -414,14 +414,14 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
 
 // ---- classification head (head.hip) --------------------------------------------
 // What the forward pass leaves for the backward pass: the statistics of x, and for every plane the mean of
-// ReLU(BN(x)), how many pixels are positive and the sum of their xhat ([n][c] each).
+// ReLU(BN(x)), how many pixels are positive and the sum of their xhat ([c][n] each: a workgroup has a channel).
 struct HeadSaved {
     float *stats, *pooled, *count, *xhat;
 };
 void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, const float *beta, HeadSaved s);
-// logits[n][k] = pooled[n][:] . w[k][:] + b[k]
+// logits[n][k] = pooled[:][n] . w[k][:] + b[k]
 void head_linear(Ctx &cx, const float *pooled, int n, int c, int classes, const float *w, const float *b, float *logits, int64_t ld);
-// d_pooled[n][c] = dl . w, dw[k][c] (+)= dl^T . pooled, db[k] (+)= sums of dl: one launch
+// d_pooled ([c][n]) = dl . w, dw[k][c] (+)= sum over images of dl * pooled, db[k] (+)= sums of dl: one launch
 void head_linear_bwd(Ctx &cx, const float *dl, int64_t ld, const float *pooled, int n, int c, int classes, const float *w,
                      float *d_pooled, float *dw, float *db, bool accumulate);
 void head_pool_bwd(Ctx &cx, View x, int c, Geo g, HeadSaved s, const float *d_pooled, float *dgamma, float *dbeta, bool accumulate,

@@ -1,6 +1,7 @@
 // Four neighbouring pixels of a plane as the unit of a streaming kernel: one 16-byte access, whatever the plane's size and
-// the tensor's alignment (16-byte accesses need dword alignment only on this hardware); the last quad of a plane whose
-// size is no multiple of four goes pixel by pixel.  Device code, but for quads_of.
+// the tensor's alignment (16-byte accesses need dword alignment only on this hardware).  Where a plane's size is no multiple
+// of four its last quad is read from four pixels before the plane's end, and the pixels that belong to the quad before it are
+// dropped: no lane goes pixel by pixel to read.  Device code, but for quads_of.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -15,21 +16,45 @@ namespace {
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef f4 f4_any __attribute__((aligned(4)));
 
-// Pixels i .. i+3 of a plane of which `left` > 0 exist; what lies beyond reads as zero and is not written.
-__device__ __forceinline__ f4 load4(const float *p, int left) {
-    if (left >= 4) return *reinterpret_cast<const f4_any *>(p);
-    f4 v = {p[0], left > 1 ? p[1] : 0.f, left > 2 ? p[2] : 0.f, 0.f};
+// Pixels i + from .. i + end - 1 of a plane are the quad's own; i .. i + 3 are in the plane where end is 4.
+struct QuadAt {
+    int i, from, end;
+    __device__ __forceinline__ bool owns(int j) const { return j >= from && j < end; }
+};
+// Quad k of a plane of hw pixels; WHOLE: hw is a multiple of four.
+template <bool WHOLE>
+__device__ __forceinline__ QuadAt quad_at(int k, int hw) {
+    if (WHOLE) return QuadAt{4 * k, 0, 4};
+    const int i = max(0, min(4 * k, hw - 4));
+    return QuadAt{i, 4 * k - i, min(4, hw - i)};
+}
+
+// (pixels that are not the quad's own read as zero and are not written)
+template <bool WHOLE>
+__device__ __forceinline__ f4 load4(const float *plane, QuadAt q) {
+    if (WHOLE) return *reinterpret_cast<const f4_any *>(plane + q.i);
+    f4 v = {0.f, 0.f, 0.f, 0.f};
+    if (q.end == 4) {
+        v = *reinterpret_cast<const f4_any *>(plane + q.i);
+#pragma unroll
+        for (int j = 0; j < 3; ++j) v[j] = j < q.from ? 0.f : v[j];
+    } else {  // a plane of fewer than four pixels
+#pragma unroll
+        for (int j = 0; j < 3; ++j) v[j] = j < q.end ? plane[j] : 0.f;
+    }
     return v;
 }
-__device__ __forceinline__ void store4(float *p, int left, f4 v) {
-    if (left >= 4) {
-        *reinterpret_cast<f4_any *>(p) = v;
+template <bool WHOLE>
+__device__ __forceinline__ void store4(float *plane, QuadAt q, f4 v) {
+    if (WHOLE || (q.from == 0 && q.end == 4)) {
+        *reinterpret_cast<f4_any *>(plane + q.i) = v;
         return;
     }
-    p[0] = v.x;
-    if (left > 1) p[1] = v.y;
-    if (left > 2) p[2] = v.z;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (q.owns(j)) plane[q.i + j] = v[j];
 }
+
 // Sum over the 64 lanes, in every lane.
 __device__ __forceinline__ double wave_total(double v) {
 #pragma unroll
@@ -38,6 +63,41 @@ __device__ __forceinline__ double wave_total(double v) {
         v += __hiloint2double(hi, lo);
     }
     return v;
+}
+// The same in fp32 by lane moves within the register file (about 50 cycles; a shuffle through LDS costs that for each of six
+// steps): rows of 16 lanes first, then the rows.
+__device__ __forceinline__ float wave_total(float v) {
+#define RVN_STEP(ctrl, rows) v += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), ctrl, rows, 0xf, false))
+    RVN_STEP(0x111, 0xf);  // row_shr 1, 2, 4, 8: the last lane of each row has the row's
+    RVN_STEP(0x112, 0xf);
+    RVN_STEP(0x114, 0xf);
+    RVN_STEP(0x118, 0xf);
+    RVN_STEP(0x142, 0xa);  // row_bcast 15 and 31: lane 63 has all
+    RVN_STEP(0x143, 0xc);
+#undef RVN_STEP
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// combine(v, w) over the 2^shift neighbouring lanes of each team (shift <= 6, the same in all lanes), in every lane: up to 16
+// lanes by moves within a row of 16 -- swapped neighbours, swapped pairs, then mirrored halves and rows, whose parts hold one
+// value each by then.
+template <typename Combine>
+__device__ __forceinline__ uint32_t team_combine(uint32_t v, int shift, Combine combine) {
+#define RVN_MOVE(ctrl) (uint32_t) __builtin_amdgcn_update_dpp((int)v, (int)v, ctrl, 0xf, 0xf, true)
+    if (shift >= 1) v = combine(v, RVN_MOVE(0xb1));   // quad_perm 1 0 3 2
+    if (shift >= 2) v = combine(v, RVN_MOVE(0x4e));   // quad_perm 2 3 0 1
+    if (shift >= 3) v = combine(v, RVN_MOVE(0x141));  // row_half_mirror
+    if (shift >= 4) v = combine(v, RVN_MOVE(0x140));  // row_mirror
+#undef RVN_MOVE
+    if (shift >= 5) v = combine(v, (uint32_t)__shfl_xor((int)v, 16, 64));
+    if (shift >= 6) v = combine(v, (uint32_t)__shfl_xor((int)v, 32, 64));
+    return v;
+}
+__device__ __forceinline__ float team_total(float v, int shift) {
+    return __uint_as_float(team_combine(__float_as_uint(v), shift, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+__device__ __forceinline__ uint32_t team_most(uint32_t v, int shift) {
+    return team_combine(v, shift, [](uint32_t a, uint32_t b) { return max(a, b); });
 }
 
 }  // namespace
