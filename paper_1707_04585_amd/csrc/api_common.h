@@ -112,8 +112,8 @@ inline size_t ckpt_codes_bytes(int c, const Geo &g) { return align_up((size_t)g.
 inline size_t ckpt_bytes(int c, const Geo &g) {
     return ckpt_codes_bytes(c, g) + (size_t)g.n * (size_t)c * (size_t)ckpt_groups(g.hw()) * 4;
 }
-// The backward workspace of a stack that stores: the plan of revnet_stack_bwd, partial sums of the BN backward passes
-// and, where the plan's room for h is too small, a buffer for one decoded layer input.
+// The backward workspace of a stack that stores: the plan of revnet_stack_bwd, whose h take the decoded inputs of the upper
+// layers, partial sums of the BN backward passes, and the decoded input of the first layer.
 struct StoredWs {
     size_t sums, xf, total;
 };

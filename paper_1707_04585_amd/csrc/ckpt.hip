@@ -7,8 +7,11 @@
 //
 // A lane works on four neighbouring pixels (quads.h): 16 bytes of fp32, 4 of codes.  Planes of any size and tensors of
 // any alignment take the same path.
+#include <algorithm>
+
 #include "fast_div.h"
 #include "kernels.h"
+#include "prep_filter.h"
 #include "quads.h"
 #include "wgrad_reduce.h"
 
@@ -51,15 +54,33 @@ __device__ __forceinline__ f4 decode(uint32_t q, float s) {
     return v;
 }
 
+// The tensors of a launch; the workgroups along x from block0 on are a tensor's.
+struct Jobs {
+    CkptTensor t[3];
+    int block0[3];
+};
+__device__ __forceinline__ CkptTensor job_of(const Jobs &jobs, int &block) {
+    const int b = block;
+    CkptTensor t = jobs.t[0];
+    if (b >= jobs.block0[1]) t = jobs.t[1], block = b - jobs.block0[1];
+    if (b >= jobs.block0[2]) t = jobs.t[2], block = b - jobs.block0[2];
+    return t;
+}
+
 // 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
 // pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
 // requests the quads of kFly images before it uses the first.
 template <bool BN, bool WHOLE>
-__global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict__ x, int64_t sn, int64_t sc, int N, int C, int HW,
-                                                        int G, FastDiv by_g, int tshift, const float *__restrict__ stats,
-                                                        int8_t *__restrict__ q, float *__restrict__ s) {
+__global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, int HW, int G, FastDiv by_g, int tshift) {
+    int block = (int)blockIdx.x;
+    const CkptTensor t = job_of(jobs, block);
+    const float *const x = t.x.p, *const stats = t.stats;
+    const int64_t sn = t.x.sn, sc = t.x.sc;
+    int8_t *const q = t.k.q;
+    float *const s = t.k.s;
+    const int C = t.c;
     constexpr int kFly = 2;
-    const int item = (int)blockIdx.x * (kThreads >> tshift) + ((int)threadIdx.x >> tshift), lane = (int)threadIdx.x & ((1 << tshift) - 1);
+    const int item = block * (kThreads >> tshift) + ((int)threadIdx.x >> tshift), lane = (int)threadIdx.x & ((1 << tshift) - 1);
     const bool live = item < C * G;
     const int ch = live ? quotient(item, by_g) : 0, group = live ? item - ch * G : 0;
     const int k0 = group * (kCkptGroup / 4) + lane;
@@ -112,15 +133,31 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const float *__restrict_
     }
 }
 
-// One lane per four pixels; blockIdx.x counts the quads of an image, blockIdx.y the images.
-template <bool WHOLE>
-__global__ __launch_bounds__(kThreads) void ckpt_load_k(const int8_t *__restrict__ q, const float *__restrict__ s, int N, int C, int HW,
-                                                        int G, FastDiv by_per, float *__restrict__ x, int64_t sn, int64_t sc) {
-    const int per = (int)by_per.d, item = (int)blockIdx.x * kThreads + (int)threadIdx.x;
+// One lane per four pixels; prep.blocks workgroups convert filters, then come by_blocks.d workgroups (the quads of an image)
+// for each of `images` images at a time.
+template <bool WHOLE, bool PREP>
+__global__ __launch_bounds__(kThreads) void ckpt_load_k(const Jobs jobs, int N, int HW, int G, FastDiv by_per, FastDiv by_blocks, int images,
+                                                        const PrepArgs prep) {
+    int block = (int)blockIdx.x;
+    if (PREP) {
+        if (block < prep.blocks) {
+            prep_filter_body(prep, block);
+            return;
+        }
+        block -= prep.blocks;
+    }
+    const int n0 = quotient(block, by_blocks);
+    block -= n0 * (int)by_blocks.d;
+    const CkptTensor t = job_of(jobs, block);
+    const int8_t *const q = t.k.q;
+    const float *const s = t.k.s;
+    float *const x = t.x.p;
+    const int64_t sn = t.x.sn, sc = t.x.sc;
+    const int C = t.c, per = (int)by_per.d, item = block * kThreads + (int)threadIdx.x;
     if (item >= C * per) return;
     const int ch = quotient(item, by_per), k = item - ch * per;
     const QuadAt at = quad_at<WHOLE>(k, HW);
-    for (int n = (int)blockIdx.y; n < N; n += (int)gridDim.y) {
+    for (int n = n0; n < N; n += images) {
         const int64_t plane = (int64_t)n * C + ch;
         const uint32_t word = load_codes<WHOLE>(q + plane * HW, at);
         store4<WHOLE>(x + (int64_t)n * sn + (int64_t)ch * sc, at, decode(word, s[plane * G + k / (kCkptGroup / 4)]));
@@ -362,25 +399,49 @@ int ckpt_bn_splits(int c, const Geo &g) {
 
 }  // namespace
 
-void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k) {
-    const int hw = g.hw(), G = ckpt_groups(hw);
-    const double planes = (double)g.n * c;
-    if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
-    int tshift = 0;  // lanes of a group: 16, or as many as a smaller plane has quads, rounded up to a power of two
-    while (tshift < 4 && (4 << tshift) < hw) ++tshift;
-    const int pairs = (g.n + 1) / 2;
-    const dim3 grid(blocks_for((int64_t)c * G, kThreads >> tshift), (unsigned)(pairs < 65535 ? pairs : 65535));
-    const bool whole = hw % 4 == 0;
-    cx.run(stats ? (whole ? ckpt_save_k<true, true> : ckpt_save_k<true, false>) : (whole ? ckpt_save_k<false, true> : ckpt_save_k<false, false>),
-           grid, dim3(kThreads), 0, x.p, x.sn, x.sc, g.n, c, hw, G, fast_div(G), tshift, stats, k.q, k.s);
+// Job list with `blocks_of(c)` workgroups a tensor; *blocks, *bytes: in all.
+template <typename BlocksOf>
+static Jobs make_jobs(const CkptTensor *t, int count, Geo g, BlocksOf blocks_of, unsigned *blocks, double *bytes) {
+    Jobs j{};
+    *blocks = 0;
+    *bytes = 0.0;
+    for (int i = 0; i < 3; ++i) {
+        j.t[i] = t[i < count ? i : 0];
+        j.block0[i] = i < count ? (int)*blocks : 0x7fffffff;
+        if (i >= count) continue;
+        *blocks += blocks_of(t[i].c);
+        *bytes += (double)g.n * t[i].c * (5.0 * g.hw() + 4.0 * ckpt_groups(g.hw()));
+    }
+    return j;
 }
 
-void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out) {
+void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g) {
+    const int hw = g.hw(), G = ckpt_groups(hw);
+    int tshift = 0;  // lanes of a group: 16, or as many as a smaller plane has quads, rounded up to a power of two
+    while (tshift < 4 && (4 << tshift) < hw) ++tshift;
+    unsigned blocks;
+    double bytes;
+    const Jobs jobs = make_jobs(t, count, g, [&](int c) { return blocks_for((int64_t)c * G, kThreads >> tshift); }, &blocks, &bytes);
+    if (!cx.launch(K_CKPT, bytes)) return;
+    const int pairs = (g.n + 1) / 2;
+    const bool whole = hw % 4 == 0, bn = t[0].stats != nullptr;  // (of all tensors or of none)
+    cx.run(bn ? (whole ? ckpt_save_k<true, true> : ckpt_save_k<true, false>) : (whole ? ckpt_save_k<false, true> : ckpt_save_k<false, false>),
+           dim3(blocks, (unsigned)(pairs < 65535 ? pairs : 65535)), dim3(kThreads), 0, jobs, g.n, hw, G, fast_div(G), tshift);
+}
+
+void ckpt_load(Ctx &cx, const CkptTensor *t, int count, Geo g, const PrepArgs *carry, double carry_bytes) {
     const int hw = g.hw(), G = ckpt_groups(hw), per = quads_of(hw);
-    const double planes = (double)g.n * c;
-    if (!cx.launch(K_CKPT, planes * (5.0 * hw + 4.0 * G))) return;
-    const dim3 grid(blocks_for((int64_t)c * per, kThreads), (unsigned)(g.n < 65535 ? g.n : 65535));
-    cx.run(hw % 4 == 0 ? ckpt_load_k<true> : ckpt_load_k<false>, grid, dim3(kThreads), 0, k.q, k.s, g.n, c, hw, G, fast_div(per), out.p, out.sn, out.sc);
+    unsigned blocks;
+    double bytes;
+    const Jobs jobs = make_jobs(t, count, g, [&](int c) { return blocks_for((int64_t)c * per, kThreads); }, &blocks, &bytes);
+    if (!cx.launch(K_CKPT, bytes + carry_bytes)) return;
+    PrepArgs prep{};
+    if (carry) prep = *carry;
+    const int images = (int)std::min<int64_t>(g.n, (1 << 30) / blocks);
+    const dim3 grid((unsigned)images * blocks + (unsigned)prep.blocks);
+    const bool whole = hw % 4 == 0;
+    cx.run(prep.blocks > 0 ? (whole ? ckpt_load_k<true, true> : ckpt_load_k<false, true>) : (whole ? ckpt_load_k<true, false> : ckpt_load_k<false, false>),
+           grid, dim3(kThreads), 0, jobs, g.n, hw, G, fast_div(per), fast_div((int)blocks), images, prep);
 }
 
 size_t ckpt_bn_scratch_floats(int c, const Geo &g) { return (size_t)c * ckpt_bn_splits(c, g) * 4; }

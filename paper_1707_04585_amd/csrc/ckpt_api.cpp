@@ -45,7 +45,8 @@ int revnet_ckpt_save(const rvn_tensor *x, const float *stats, void *ckpt, size_t
     if (int rc = check_ckpt_tensor("x", x, ckpt, have, &c, &g)) return rc;
     Ctx cx;
     cx.stream = static_cast<hipStream_t>(hip_stream);
-    ckpt_save(cx, view_of(x), c, g, stats, ckpt_of(ckpt, c, g));
+    const CkptTensor t{view_of(x), c, stats, ckpt_of(ckpt, c, g)};
+    ckpt_save(cx, &t, 1, g);
     return finish(cx);
 }
 
@@ -55,7 +56,8 @@ int revnet_ckpt_load(const void *ckpt, size_t have, const rvn_tensor *x, void *h
     if (int rc = check_ckpt_tensor("x", x, ckpt, have, &c, &g)) return rc;
     Ctx cx;
     cx.stream = static_cast<hipStream_t>(hip_stream);
-    ckpt_load(cx, ckpt_of(const_cast<void *>(ckpt), c, g), c, g, view_of(x));  // (the checkpoint is read only)
+    const CkptTensor t{view_of(x), c, nullptr, ckpt_of(const_cast<void *>(ckpt), c, g)};  // (the checkpoint is read only)
+    ckpt_load(cx, &t, 1, g);
     return finish(cx);
 }
 

@@ -403,9 +403,17 @@ struct Ckpt {
 };
 constexpr int kCkptGroup = RVN_CKPT_GROUP;
 inline int ckpt_groups(int hw) { return (hw + kCkptGroup - 1) / kCkptGroup; }
-// stats: null, or the four statistics arrays of the BN layer that reads x, whose ReLU decisions are then kept.
-void ckpt_save(Ctx &cx, View x, int c, Geo g, const float *stats, Ckpt k);
-void ckpt_load(Ctx &cx, Ckpt k, int c, Geo g, View out);
+// Up to three tensors of one geometry are saved, or loaded, by a launch.  stats (save only): null, or the four statistics
+// arrays of the BN layer that reads x, whose ReLU decisions are then kept.
+struct CkptTensor {
+    View x;
+    int c;
+    const float *stats;
+    Ckpt k;
+};
+void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g);
+// carry: a filter conversion that rides in the launch.
+void ckpt_load(Ctx &cx, const CkptTensor *t, int count, Geo g, const PrepArgs *carry = nullptr, double carry_bytes = 0.0);
 // bn_relu_bwd with x read from a checkpoint and da anywhere; scratch: ckpt_bn_scratch_floats(c, g) floats.  `carry`, out16: as there
 // (out16 needs no alignment here; no skip).
 size_t ckpt_bn_scratch_floats(int c, const Geo &g);

@@ -205,17 +205,10 @@ StorePlan make_store_plan(const rvn_block_desc &d, const Geo &g) {
 }
 
 StoredWs stored_bwd_ws(const Plan &p, const Geo &g) {
-    size_t sums = 0, widest = 0;
-    for (int l = 0; l < p.L; ++l) {
-        sums = std::max(sums, ckpt_bn_scratch_floats(p.layers[l].cin, g));
-        widest = std::max(widest, (size_t)p.layers[l].cin);
-    }
-    StoredWs w{p.total, p.h[0], align_up(p.total + sums * 4)};
-    const size_t need = (size_t)g.pixels() * widest * 4;
-    if (p.g[0] - p.h[0] < need) {
-        w.xf = w.total;
-        w.total = align_up(w.xf + need);
-    }
+    size_t sums = 0;
+    for (int l = 0; l < p.L; ++l) sums = std::max(sums, ckpt_bn_scratch_floats(p.layers[l].cin, g));
+    StoredWs w{p.total, align_up(p.total + sums * 4), 0};
+    w.total = align_up(w.xf + (size_t)g.pixels() * p.layers[0].cin * 4);
     return w;
 }
 
@@ -372,6 +365,7 @@ const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
         prep[l] = FilterPrep{p.conv_w[l], pl.layers[l].cin, pl.layers[l].cout, pl.layers[l].ks, b.wq_f[l], b.wq_b[l]};
     // The conversion rides in the first statistics launch of the function.
     double prep_bytes = 0.0;
+    CkptTensor kept[3];
     // A forward pass of small narrow layers does without: the launch that would carry it is then not needed.
     bool convert = !(ep == EP_ADD && d.conv_dtype == RVN_BF16 && !ahead && cx.emitted.p == x.p);
     for (int l = 0; l < pl.L && !convert; ++l)
@@ -405,9 +399,10 @@ const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
         } else {
             conv_fwd(cx, cur, scale_shift, d.conv_dtype, p.conv_w[l], wq, ly.cin, ly.cout, ly.ks, g, ep, r, out, b.conv_scratch);
         }
-        // (after the convolution: a deferred merge leaves the statistics there only now)
-        if (keep) ckpt_save(cx, in, ly.cin, g, b.stats[l], keep[l]);
+        if (keep) kept[l] = CkptTensor{in, ly.cin, b.stats[l], keep[l]};
     }
+    // (every layer's input is still there: the function's own, which no layer writes, and the h of this function)
+    if (keep) ckpt_save(cx, kept, pl.L, g);
     return stats0;
 }
 
@@ -531,9 +526,9 @@ StoredFunc stored_func(const Plan &pl, const StorePlan &sp, const Bufs &b, char 
     return f;
 }
 
-// func_backward with every layer's input read from its checkpoint: decoded for the two products of a layer, straight from
-// the codes for its BN backward pass.  sums, xf: see StoredWs.  Nothing has converted the function's filters: that
-// is the first launch.
+// func_backward with every layer's input read from its checkpoint: decoded for the two products of a layer (all layers in one
+// launch, which also converts the function's filters), straight from the codes for its BN backward pass.  sums, xf: see
+// StoredWs.
 void func_backward_stored(Ctx &cx, const rvn_block_desc &d, const Plan &pl, const StoredFunc &f, Geo g, const rvn_func_params &p,
                           View upstream, const rvn_func_grads &gr, bool accumulate, View skip, View out, float *sums, float *xf) {
     const Bufs &b = f.b;
@@ -542,14 +537,19 @@ void func_backward_stored(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
         prep[l] = FilterPrep{p.conv_w[l], pl.layers[l].cin, pl.layers[l].cout, pl.layers[l].ks, nullptr, b.wq_b[l]};
     double prep_bytes = 0.0;
     const PrepArgs pa = plan_filter_prep(prep, pl.L, g, &prep_bytes);
-    if (pa.jobs > 0) prep_filters_bf16(cx, pa, prep_bytes);
+    View in[3];
+    CkptTensor kept[3];
+    for (int l = 0; l < pl.L; ++l) {
+        in[l] = dense_view(l > 0 ? b.h[l - 1] : xf, pl.layers[l].cin, g);
+        kept[l] = CkptTensor{in[l], pl.layers[l].cin, nullptr, f.k[l]};
+    }
+    ckpt_load(cx, kept, pl.L, g, &pa, prep_bytes);
     View dh = upstream;
     const uint16_t *dh16 = nullptr;
     int cur = 0;
     for (int l = pl.L - 1; l >= 0; --l) {
         const Layer &ly = pl.layers[l];
-        const View xl = dense_view(xf, ly.cin, g);
-        ckpt_load(cx, f.k[l], ly.cin, g, xl);
+        const View xl = in[l];
         WgradReduce red;
         float *da = b.g[cur];
         const float *const scale_shift = b.stats[l] + 2 * ly.cin;
@@ -574,7 +574,7 @@ void func_backward_stored(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
             const Layer &below = pl.layers[l - 1];
             uint16_t *const as16 = reinterpret_cast<uint16_t *>(b.g[cur ^ 1]);
             const bool to16 = d.conv_dtype == RVN_BF16 && g.hw() % 4 == 0 &&
-                              conv_dgrad_wgrad_takes_bf16_dh(dense_view(xf, below.cin, g), as16, b.wq_b[l - 1], below.cin, below.cout,
+                              conv_dgrad_wgrad_takes_bf16_dh(in[l - 1], as16, b.wq_b[l - 1], below.cin, below.cout,
                                                              below.ks, g, b.wgrad_scratch, da, b.conv_scratch);
             ckpt_bn_relu_bwd(cx, f.k[l], dav, ly.cin, g, b.stats[l], sums, gr.d_bn_gamma[l], gr.d_bn_beta[l], accumulate, nullptr, dav,
                              &red, to16 ? as16 : nullptr);
