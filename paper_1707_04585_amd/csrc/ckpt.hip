@@ -35,10 +35,13 @@ __device__ __forceinline__ uint32_t load_codes(const int8_t *plane, QuadAt q) {
     for (int j = 0; j < 3; ++j) v |= j < q.end ? (uint32_t)(uint8_t)plane[j] << (8 * j) : 0u;
     return v;
 }
-template <bool WHOLE>
+// FAR: nothing reads the codes soon, they shall not push what the caches hold out of them
+template <bool WHOLE, bool FAR>
 __device__ __forceinline__ void store_codes(int8_t *plane, QuadAt q, uint32_t word) {
     if (WHOLE || (q.from == 0 && q.end == 4)) {
-        *reinterpret_cast<u32_any *>(plane + q.i) = word;
+        u32_any *const to = reinterpret_cast<u32_any *>(plane + q.i);
+        if (FAR) __builtin_nontemporal_store(word, to);
+        else *to = word;
         return;
     }
 #pragma unroll
@@ -70,7 +73,7 @@ __device__ __forceinline__ CkptTensor job_of(const Jobs &jobs, int &block) {
 // 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
 // pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
 // requests the quads of kFly images before it uses the first.
-template <bool BN, bool WHOLE>
+template <bool BN, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, int HW, int G, FastDiv by_g, int tshift) {
     int block = (int)blockIdx.x;
     const CkptTensor t = job_of(jobs, block);
@@ -126,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, 
                     word |= ((uint32_t)(int)c & 0xffu) << (8 * j);
                 }
                 if (!finite) word = 0;
-                store_codes<WHOLE>(q + plane * HW, at[h], word);
+                store_codes<WHOLE, FAR>(q + plane * HW, at[h], word);
             }
             if (live && lane == 0) s[plane * G + group] = finite ? step : __uint_as_float(0x7fc00000u);
         }
@@ -415,7 +418,7 @@ static Jobs make_jobs(const CkptTensor *t, int count, Geo g, BlocksOf blocks_of,
     return j;
 }
 
-void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g) {
+void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g, bool far) {
     const int hw = g.hw(), G = ckpt_groups(hw);
     int tshift = 0;  // lanes of a group: 16, or as many as a smaller plane has quads, rounded up to a power of two
     while (tshift < 4 && (4 << tshift) < hw) ++tshift;
@@ -425,7 +428,10 @@ void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g) {
     if (!cx.launch(K_CKPT, bytes)) return;
     const int pairs = (g.n + 1) / 2;
     const bool whole = hw % 4 == 0, bn = t[0].stats != nullptr;  // (of all tensors or of none)
-    cx.run(bn ? (whole ? ckpt_save_k<true, true> : ckpt_save_k<true, false>) : (whole ? ckpt_save_k<false, true> : ckpt_save_k<false, false>),
+    void (*kernel)(const Jobs, int, int, int, FastDiv, int) = whole ? ckpt_save_k<false, true, false> : ckpt_save_k<false, false, false>;
+    if (bn && far) kernel = whole ? ckpt_save_k<true, true, true> : ckpt_save_k<true, false, true>;
+    else if (bn) kernel = whole ? ckpt_save_k<true, true, false> : ckpt_save_k<true, false, false>;
+    cx.run(kernel,
            dim3(blocks, (unsigned)(pairs < 65535 ? pairs : 65535)), dim3(kThreads), 0, jobs, g.n, hw, G, fast_div(G), tshift);
 }
 
@@ -437,7 +443,7 @@ void ckpt_load(Ctx &cx, const CkptTensor *t, int count, Geo g, const PrepArgs *c
     if (!cx.launch(K_CKPT, bytes + carry_bytes)) return;
     PrepArgs prep{};
     if (carry) prep = *carry;
-    const int images = (int)std::min<int64_t>(g.n, (1 << 30) / blocks);
+    const int images = (int)std::max<int64_t>(1, std::min<int64_t>(g.n, (1 << 30) / blocks));
     const dim3 grid((unsigned)images * blocks + (unsigned)prep.blocks);
     const bool whole = hw % 4 == 0;
     cx.run(prep.blocks > 0 ? (whole ? ckpt_load_k<true, true> : ckpt_load_k<false, true>) : (whole ? ckpt_load_k<true, false> : ckpt_load_k<false, false>),

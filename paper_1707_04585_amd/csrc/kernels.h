@@ -411,7 +411,10 @@ struct CkptTensor {
     const float *stats;
     Ckpt k;
 };
-void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g);
+// far: the codes are read only after much else has passed through the caches (a stack's backward pass).  The convolutions of 12
+// bottleneck blocks of 56x56 then lose 0.15 ms to the saving between them instead of 0.42 (of 2.74); a checkpoint read back
+// at once costs 59 us instead of 51 (64x128x56x56, save and load), hence only there.  (Only with stats.)
+void ckpt_save(Ctx &cx, const CkptTensor *t, int count, Geo g, bool far = false);
 // carry: a filter conversion that rides in the launch.
 void ckpt_load(Ctx &cx, const CkptTensor *t, int count, Geo g, const PrepArgs *carry = nullptr, double carry_bytes = 0.0);
 // bn_relu_bwd with x read from a checkpoint and da anywhere; scratch: ckpt_bn_scratch_floats(c, g) floats.  `carry`, out16: as there

@@ -402,7 +402,7 @@ const float *func_forward(Ctx &cx, const rvn_block_desc &d, const Plan &pl, cons
         if (keep) kept[l] = CkptTensor{in, ly.cin, b.stats[l], keep[l]};
     }
     // (every layer's input is still there: the function's own, which no layer writes, and the h of this function)
-    if (keep) ckpt_save(cx, kept, pl.L, g);
+    if (keep) ckpt_save(cx, kept, pl.L, g, true);
     return stats0;
 }
 
