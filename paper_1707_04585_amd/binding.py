@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -287,15 +288,32 @@ def _dtype_name(dtype):
     return name
 
 
-def _matrix(t, name):
+# The bytes of an rvn_tensor or rvn_matrix, for entry points with a signature: they take an address, ctypes passes that of
+# the bytes, and packing them is quicker than filling a structure field by field.
+_pack_tensor = struct.Struct("9q").pack
+_pack_matrix = struct.Struct("qi4x3q").pack
+
+
+def _tensor_arg(t):
+    if t is None or isinstance(t, rvn_tensor):
+        return None if t is None else C.byref(t)
+    return _pack_tensor(t.data_ptr(), *t.shape, *t.stride())
+
+
+def _channels(t):
+    return t.c if isinstance(t, rvn_tensor) else t.shape[1]
+
+
+def _matrix_arg(t, name):
+    """-> (argument, rows)"""
     if t is None or isinstance(t, rvn_matrix):
-        return t
+        return (None, 0) if t is None else (C.byref(t), t.rows)
     rows, cols = t.shape
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"the columns of {name} must be contiguous")
     dtype = {"float32": F32, "bfloat16": BF16}.get(_dtype_name(t.dtype), -1)
-    return rvn_matrix(t.data_ptr(), dtype, rows, cols, ld if rows > 1 else max(ld, cols))
+    return _pack_matrix(t.data_ptr(), dtype, rows, cols, ld if rows > 1 else max(ld, cols)), rows
 
 
 def _vector(t, name, count, dtype="float32"):
@@ -305,10 +323,6 @@ def _vector(t, name, count, dtype="float32"):
     if _dtype_name(t.dtype) != dtype or t.numel() != count or not t.is_contiguous():
         raise ValueError(f"{name} must be {count} contiguous elements of {dtype}")
     return t.data_ptr()
-
-
-def _by_ref(t):
-    return None if t is None else C.byref(t)
 
 
 def _stream(stream):
@@ -575,13 +589,12 @@ def revnet_ckpt_bytes(n, c, h, w):
 
 def revnet_ckpt_save(x, stats, ckpt, stream=None):
     """stats: None, or a [4, c] tensor (mean, rstd, scale, shift)."""
-    tx = _tensor(x)
-    _check(load_library().revnet_ckpt_save(C.byref(tx), _vector(stats, "stats", 4 * tx.c), *_ws(ckpt), _stream(stream)))
+    _check(load_library().revnet_ckpt_save(_tensor_arg(x), stats if stats is None else _vector(stats, "stats", 4 * _channels(x)),
+                                           *_ws(ckpt), _stream(stream)))
 
 
 def revnet_ckpt_load(ckpt, x, stream=None):
-    tx = _tensor(x)
-    _check(load_library().revnet_ckpt_load(*_ws(ckpt), C.byref(tx), _stream(stream)))
+    _check(load_library().revnet_ckpt_load(*_ws(ckpt), _tensor_arg(x), _stream(stream)))
 
 
 def revnet_ckpt_bn_relu_workspace_bytes(n, c, h, w):
@@ -591,11 +604,9 @@ def revnet_ckpt_bn_relu_workspace_bytes(n, c, h, w):
 
 
 def revnet_ckpt_bn_relu_bwd(ckpt, stats, da, skip, dx, d_gamma, d_beta, accumulate, ws, stream=None):
-    ta, tx = _tensor(da), _tensor(dx)
-    ts = None if skip is None else _tensor(skip)
-    c = ta.c
+    c = _channels(da)
     _check(load_library().revnet_ckpt_bn_relu_bwd(
-        *_ws(ckpt), _vector(stats, "stats", 4 * c), C.byref(ta), _by_ref(ts), C.byref(tx), _vector(d_gamma, "d_gamma", c),
+        *_ws(ckpt), _vector(stats, "stats", 4 * c), _tensor_arg(da), _tensor_arg(skip), _tensor_arg(dx), _vector(d_gamma, "d_gamma", c),
         _vector(d_beta, "d_beta", c), int(accumulate), *_ws(ws), _stream(stream)))
 
 
@@ -678,15 +689,15 @@ def revnet_head_workspace_bytes(desc, n, h, w):
 
 
 def revnet_head_fwd(desc, x, params, logits, saved, stream=None):
-    d, p, tx, tl = _desc(desc), pack_head(params), _tensor(x), _matrix(logits, "logits")
-    _check(load_library().revnet_head_fwd(C.byref(d), C.byref(tx), C.byref(p), _by_ref(tl), *_ws(saved), _stream(stream)))
+    d, p = _desc(desc), pack_head(params)
+    _check(load_library().revnet_head_fwd(C.byref(d), _tensor_arg(x), C.byref(p), _matrix_arg(logits, "logits")[0], *_ws(saved),
+                                          _stream(stream)))
 
 
 def revnet_head_bwd(desc, x, saved, d_logits, params, dx, grads, accumulate_wgrads, ws, stream=None):
     d, p, g = _desc(desc), pack_head(params), pack_head(grads)
-    tx, tl, td = _tensor(x), _matrix(d_logits, "d_logits"), _tensor(dx)
-    _check(load_library().revnet_head_bwd(C.byref(d), C.byref(tx), *_ws(saved), _by_ref(tl), C.byref(p), C.byref(td), C.byref(g),
-                                          int(accumulate_wgrads), *_ws(ws), _stream(stream)))
+    _check(load_library().revnet_head_bwd(C.byref(d), _tensor_arg(x), *_ws(saved), _matrix_arg(d_logits, "d_logits")[0], C.byref(p),
+                                          _tensor_arg(dx), C.byref(g), int(accumulate_wgrads), *_ws(ws), _stream(stream)))
 
 
 def revnet_logprob_workspace_bytes(rows, classes, top_k):
@@ -697,22 +708,20 @@ def revnet_logprob_workspace_bytes(rows, classes, top_k):
 
 def revnet_logprob_fwd(logits, labels, top_k, logprob, entropy, lse, top_ids, top_logprob, ws, stream=None):
     """With top_k == 0 top_ids and top_logprob are not looked at; any other output may be None (labels with logprob)."""
-    m = _matrix(logits, "logits")
-    rows = m.rows if m is not None else 0
+    m, rows = _matrix_arg(logits, "logits")
     if top_k == 0:
         top_ids = top_logprob = None
     _check(load_library().revnet_logprob_fwd(
-        _by_ref(m), _vector(labels, "labels", rows, "int64"), top_k, _vector(logprob, "logprob", rows), _vector(entropy, "entropy", rows),
+        m, _vector(labels, "labels", rows, "int64"), top_k, _vector(logprob, "logprob", rows), _vector(entropy, "entropy", rows),
         _vector(lse, "lse", rows), _vector(top_ids, "top_ids", rows * top_k, "int64"), _vector(top_logprob, "top_logprob", rows * top_k),
         *_ws(ws), _stream(stream)))
 
 
 def revnet_logprob_bwd(logits, labels, lse, entropy, d_logprob, d_entropy, scale, d_logits, stream=None):
-    m, d = _matrix(logits, "logits"), _matrix(d_logits, "d_logits")
-    rows = m.rows if m is not None else 0
+    m, rows = _matrix_arg(logits, "logits")
     _check(load_library().revnet_logprob_bwd(
-        _by_ref(m), _vector(labels, "labels", rows, "int64"), _vector(lse, "lse", rows), _vector(entropy, "entropy", rows),
-        _vector(d_logprob, "d_logprob", rows), _vector(d_entropy, "d_entropy", rows), scale, _by_ref(d), _stream(stream)))
+        m, _vector(labels, "labels", rows, "int64"), _vector(lse, "lse", rows), _vector(entropy, "entropy", rows),
+        _vector(d_logprob, "d_logprob", rows), _vector(d_entropy, "d_entropy", rows), scale, _matrix_arg(d_logits, "d_logits")[0], _stream(stream)))
 
 
 def revnet_profile_begin():

@@ -362,6 +362,7 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
     float a0 = 0.f, a1 = 0.f;
 #pragma unroll
     for (int u = 0; u < kFusedQuads; ++u) {
+        if (u * T >= total) break;  // (uniform)
         const int e = (int)threadIdx.x + u * T;
         quad(fetch<WHOLE>(b, place<WHOLE>(b, ch, e < total ? e : 0), ch, e < total, da, dsn, dsc), c, dz[u], xm[u]);
 #pragma unroll

@@ -16,6 +16,7 @@
 // the place that the number of larger keys in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
 // wavefront takes its largest keys one by one and the lists are merged.
 #include "kernels.h"
+#include "quads.h"
 
 namespace rvn {
 
@@ -138,6 +139,12 @@ __device__ __forceinline__ Key wave_most(Key k) {
     return Key{hi, wave_most(k.hi == hi ? k.lo : 0u)};
 }
 
+// Largest of the lanes' values, none of them NaN.
+__device__ __forceinline__ float wave_largest(float v) {
+    const uint32_t most = wave_most(order_bits(v));
+    return value_of(most);
+}
+
 struct Sums {
     float m, s, t;
 };
@@ -148,10 +155,10 @@ __device__ __forceinline__ Sums join(Sums a, Sums b) {
     // (differences below -200 have a factor of 0: clamped, so that 0 * -infinity cannot arise)
     return Sums{m, a.s * fa + b.s * fb, fa * (a.t + a.s * fmaxf(da, -200.f)) + fb * (b.t + b.s * fmaxf(db, -200.f))};
 }
+// The join of the 64 lanes' sums, in every lane: to the largest m of all first, then three plain sums' worth of lane moves.
 __device__ __forceinline__ Sums wave_join(Sums v) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = join(v, Sums{__shfl_xor(v.m, o, 64), __shfl_xor(v.s, o, 64), __shfl_xor(v.t, o, 64)});
-    return v;
+    const float m = wave_largest(v.m), down = (v.m - m) * kLog2e, f = __builtin_amdgcn_exp2f(down);
+    return Sums{m, wave_total(v.s * f), wave_total(f * (v.t + v.s * fmaxf(down, -200.f)))};
 }
 
 // A team of NT threads on `length` classes of a row from class `first`: vector v of that part, its classes
@@ -301,6 +308,7 @@ __device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top
 #pragma unroll
         for (int w = 0; w < NW; ++w) count += __popcll(__ballot(seen[w] >= next));
         if (count >= top_k) bound = next;
+        if (count == top_k) break;  // (uniform) exactly these
     }
     const float least = bound <= kLowestOrder ? -INFINITY : value_of(bound);  // order bits reach `bound`: the value reaches this
     // A thread whose largest reaches the bound lists what it kept; where its second group reaches it too, the wavefront reads
@@ -425,14 +433,25 @@ __device__ __forceinline__ float log_probability(const Row &r, float x) {
     return r.nan ? __uint_as_float(0x7fc00000u) : r.empty ? -INFINITY : (x - r.m) - r.log_s;
 }
 
+// A row's label and its logit, requested before the row is read: neither depends on it.
+struct Given {
+    int64_t label;
+    float logit;
+};
 template <typename T>
-__device__ __forceinline__ void put_row(const T *row, int classes, int64_t at, Sums a, const int64_t *labels, const LogprobOut &out) {
+__device__ __forceinline__ Given given_of(const T *row, int classes, int64_t at, const int64_t *labels) {
+    Given g{RVN_NO_LABEL, 0.f};
+    if (labels) g.label = labels[at];
+    if (g.label >= 0 && g.label < classes) g.logit = Vec<T>::one(row, g.label);
+    return g;
+}
+
+__device__ __forceinline__ void put_row(int classes, int64_t at, Sums a, const Given &given, const LogprobOut &out) {
     const Row r = row_of(a);
     if (out.logprob) {
-        const int64_t label = labels[at];
         float v = __uint_as_float(0x7fc00000u);
-        if (label == RVN_NO_LABEL) v = 0.f;
-        else if (label >= 0 && label < classes) v = log_probability(r, Vec<T>::one(row, label));
+        if (given.label == RVN_NO_LABEL) v = 0.f;
+        else if (given.label >= 0 && given.label < classes) v = log_probability(r, given.logit);
         out.logprob[at] = v;
     }
     if (out.entropy) out.entropy[at] = r.empty ? 0.f : r.log_s - kLn2 * (a.t / a.s);
@@ -453,9 +472,10 @@ __global__ __launch_bounds__(kThreads) void logprob_wave_k(const T *x, int64_t r
     const int64_t at = (int64_t)blockIdx.x * (kThreads / 64) + wave;
     if (at >= rows) return;
     const Part<T> p(x, at, rows, ld, classes, 0, classes, 64);
+    const Given given = given_of(p.row, classes, at, labels);
     Top<Vec<T>::FLY> top;
     const Sums a = wave_join(stream<TOP>(p, lane, top));
-    if (lane == 0) put_row(p.row, classes, at, a, labels, out);
+    if (lane == 0) put_row(classes, at, a, given, out);
     if constexpr (TOP) {
         const Row row = row_of(a);
         team_top<T, 1>(p, lane, top, row.nan, out.top_k, lds[wave], [&](int i, Key k) { put_top(out, at, i, k, row); });
@@ -474,6 +494,8 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t r
     const int split = splits == 1 ? 0 : (int)(blockIdx.x - (unsigned)at * (unsigned)splits);
     const int first = split * share;
     const Part<T> p(x, at, rows, ld, classes, first, min(share, classes - first), NW * 64);
+    Given given{RVN_NO_LABEL, 0.f};
+    if (splits == 1) given = given_of(p.row, classes, at, labels);
     Top<Vec<T>::FLY> top;
     const Sums mine = wave_join(stream<TOP>(p, thread, top));
     if (lane == 0) parts[wave] = mine;
@@ -483,7 +505,7 @@ __global__ __launch_bounds__(NW * 64) void logprob_block_k(const T *x, int64_t r
     for (int w = 1; w < NW; ++w) a = join(a, parts[w]);
     const int64_t slot = at * splits + split;
     if (thread == 0) {
-        if (splits == 1) put_row(p.row, classes, at, a, labels, out);
+        if (splits == 1) put_row(classes, at, a, given, out);
         else sums[slot] = make_float4(a.m, a.s, a.t, 0.f);
     }
     if constexpr (TOP) {
@@ -505,6 +527,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_k(const T *x, int64_t l
     const int thread = (int)threadIdx.x, lane = thread & 63, top_k = out.top_k;
     const int64_t at = blockIdx.x;
     const Key *row_keys = keys + at * splits * top_k;
+    const Given given = given_of(x + at * ld, classes, at, labels);
     Sums a{kLowest, 0.f, 0.f};
     Key last{0u, 0u};
     if (lane < splits) {
@@ -513,7 +536,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_k(const T *x, int64_t l
         if (top_k > 0) last = row_keys[lane * top_k + top_k - 1];
     }
     a = wave_join(a);
-    if (thread == 0) put_row(x + at * ld, classes, at, a, labels, out), listed = 0;
+    if (thread == 0) put_row(classes, at, a, given, out), listed = 0;
     if (top_k == 0) return;
     const Row r = row_of(a);
     const Key bound = wave_most(last);
