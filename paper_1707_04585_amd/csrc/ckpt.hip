@@ -299,7 +299,7 @@ __device__ __forceinline__ void put_sums(const Channel &c, double sum, double su
 // The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
 template <bool SKIP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc,
-                                                            const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_chunks,
+                                                            const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_c, int chunks,
                                                             float *dgamma, float *dbeta, int accumulate, const float *skip, int64_t ksn,
                                                             int64_t ksc, float *out, int64_t osn, int64_t osc, uint16_t *out16,
                                                             const WgradReduce carry) {
@@ -308,7 +308,8 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
         wgrad_reduce_body(carry, (int)blockIdx.x, lds);
         return;
     }
-    const int bx = (int)blockIdx.x - carry.blocks, ch = quotient(bx, by_chunks), chunk = bx - ch * (int)by_chunks.d;
+    // (channels first, as the sums were formed, and from the end: what was read last is in the nearer caches)
+    const int bx = (int)blockIdx.x - carry.blocks, back = quotient(bx, by_c), ch = bx - back * b.C, chunk = chunks - 1 - back;
     const int total = b.N * (int)b.by_per.d, e0 = chunk * kFly * kThreads + (int)threadIdx.x;
     const Channel c = channel(b, ch);
     Quad q[kFly];
@@ -492,7 +493,7 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
         const dim3 grid((unsigned)(chunks * c + red.blocks));
         cx.run(skip ? (whole ? ckpt_bn_apply_k<true, true> : ckpt_bn_apply_k<true, false>)
                     : (whole ? ckpt_bn_apply_k<false, true> : ckpt_bn_apply_k<false, false>),
-               grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(chunks), dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p,
+               grid, dim3(kThreads), 0, b, da.p, da.sn, da.sc, sums, S, inv_m, fast_div(c), chunks, dgamma, dbeta, acc, kv.p, kv.sn, kv.sc, out.p,
                out.sn, out.sc, out16, red);
     }
 }
