@@ -378,19 +378,19 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
     p.J = (p.per + (1 << p.tshift) - 1) >> p.tshift;
     const int at_once = 64 >> p.tshift;
     auto steps = [&](int waves) { return (g.n + waves * at_once - 1) / (waves * at_once); };
-    // The fixed work of a wavefront (sums over lanes, statistics) outweighs a few quads a lane: as few wavefronts a channel as
-    // keep its quads in registers, eight a lane, and give every SIMD two of them.
-    constexpr int kWavesWanted = 8192;
+    // As few wavefronts a channel as keep its quads in registers, eight a lane, and fill the chip with eight a SIMD.
     int waves = 1;
-    while (waves < 16 && ((int64_t)c * waves < kWavesWanted || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
+    while (waves < 16 && ((int64_t)c * waves < 8192 || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
     p.steps = steps(waves);
-    const bool held = (int64_t)p.steps * p.J <= 8, whole = g.hw() % 4 == 0;
+    const int64_t held = (int64_t)p.steps * p.J;
+    const bool whole = g.hw() % 4 == 0;
 #define RVN_POOL(TH, HELD)                                                                                                     \
     cx.run(whole ? head_pool_k<TH, HELD, true> : head_pool_k<TH, HELD, false>, dim3((unsigned)c), dim3(TH), 0, x.p, x.sn, x.sc, p, eps, \
            gamma, beta, s.stats, s.pooled, s.count, s.xhat)
-    if (!held) RVN_POOL(1024, 0);
+    if (held > 8) RVN_POOL(1024, 0);
     else if (waves == 1) RVN_POOL(64, 8);
-    else if (waves == 4) RVN_POOL(256, 8);
+    else if (waves == 4 && held > 2) RVN_POOL(256, 8);
+    else if (waves == 4) RVN_POOL(256, 2);
     else RVN_POOL(1024, 8);
 #undef RVN_POOL
 }
