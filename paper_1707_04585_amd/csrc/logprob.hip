@@ -611,11 +611,15 @@ struct Shape {
     int splits, share;   // else workgroups a row, and the classes of each
 };
 
-// Rows up to 8 KB go to one wavefront each; longer ones to a workgroup, or to several where there are fewer rows than
-// compute units and each still has 16 KB to read.
-Shape shape_of(int64_t rows, int classes, int size) {
+// Rows up to 8 KB go to one wavefront each, and up to 32 KB where they are so many that each SIMD has two: a wavefront needs
+// no barrier, where a workgroup waits for its slowest at every join.  (8192 x 4200, 5 top classes: 35.1 us by workgroups, 24.1
+// by wavefronts in bf16, 37.3 and 28.7 in fp32; 2048 x 15000 bf16 20.3 and 18.4; 3000 x 32003 bf16 47.4 both, without top
+// classes 42.1 and 44.9.)  The more top classes, the more of a wavefront's 64 threads have to read their vectors again, which a
+// workgroup spreads over 256: 16 of 2048 x 15000 cost 21.9 and 22.4, 32 of them 24.2 and 31.8.
+// Else a row goes to a workgroup, or to several where there are fewer rows than compute units and each still has 16 KB to read.
+Shape shape_of(int64_t rows, int classes, int size, int top_k) {
     const int64_t bytes = (int64_t)classes * size;
-    if (bytes <= 8192) return Shape{true, 1, classes};
+    if (bytes <= 8192 || (rows >= 2048 && bytes <= 32768 && top_k <= 12)) return Shape{true, 1, classes};
     if (rows >= 256) return Shape{false, 1, classes};
     int64_t splits = (512 + rows - 1) / rows;
     const int64_t most = (bytes + 16383) / 16384;
@@ -629,7 +633,7 @@ Shape shape_of(int64_t rows, int classes, int size) {
 template <typename T>
 void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch) {
     const T *p = static_cast<const T *>(x.p);
-    const Shape s = shape_of(x.rows, x.classes, (int)sizeof(T));
+    const Shape s = shape_of(x.rows, x.classes, (int)sizeof(T), out.top_k);
     const double bytes = (double)x.rows * ((double)x.classes * sizeof(T) + 20.0 + 12.0 * out.top_k);
     if (!cx.launch(K_LOGPROB, bytes, 5.0 * (double)x.rows * x.classes)) return;
     if (s.wave) {
@@ -666,7 +670,7 @@ void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse,
 size_t logprob_scratch_bytes(int64_t rows, int classes, int top_k) {
     size_t most = 0;  // of the two types' shapes
     for (int size = 2; size <= 4; size += 2) {
-        const Shape s = shape_of(rows, classes, size);
+        const Shape s = shape_of(rows, classes, size, top_k);
         const size_t need = s.splits > 1 ? (size_t)rows * s.splits * (sizeof(float4) + (size_t)top_k * sizeof(Key)) : 0;
         most = most > need ? most : need;
     }

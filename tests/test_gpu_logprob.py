@@ -118,6 +118,37 @@ def test_masks_ties_and_values_that_are_no_numbers(classes, bf16):
     assert got["entropy"][0] == 0 and got["lse"][0] == -np.inf and got["logprob"][3] == -np.inf and got["logprob"][7] == 0
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("classes", [2600, 5001, 8191])
+def test_many_rows_of_middle_length(classes, bf16):
+    """So many rows that each of these goes to one wavefront, or (13 top classes) to a workgroup: the values that can go wrong
+    among the first and last rows, and both ways agree on the classes of all."""
+    import torch
+    rng = np.random.default_rng(classes)
+    rows, some = 2051, 12
+    t, _ = logits(rng, rows, classes, bf16, pad=1, offset=1)
+    lowest = torch.finfo(t.dtype).min
+    t[0] = -torch.inf
+    t[1] = lowest
+    t[2, : classes - 1] = -torch.inf
+    t[3] = 1.25
+    t[4] = torch.as_tensor(rng.integers(0, 3, classes).astype(np.float32)).cuda()
+    t[5, classes // 2] = torch.nan
+    t[6, classes - 1] = torch.inf
+    t[7, 1::2] = lowest
+    t[8] *= 100
+    t[rows - 1, : classes - 5] = -torch.inf
+    t[rows - 2, 5] = torch.nan
+    lab = labels_of(rng, rows, classes)
+    lab[2], lab[9] = classes - 1, -1
+    out, wide = (forward(t, torch.as_tensor(lab).cuda(), k) for k in (12, 13))
+    torch.cuda.synchronize()
+    for part in (slice(0, some), slice(rows - some, rows)):
+        check({k: v[part] for k, v in out.host().items()}, R.logprob(t[part].float().cpu().numpy(), lab[part], 12))
+        check({k: v[part] for k, v in wide.host().items()}, R.logprob(t[part].float().cpu().numpy(), lab[part], 13))
+    assert torch.equal(out.ids, wide.ids[:, :12])
+
+
 def test_outputs_that_are_not_asked_for():
     import torch
     import paper_1707_04585_amd as rv
