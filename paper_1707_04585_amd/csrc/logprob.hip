@@ -562,7 +562,7 @@ __global__ __launch_bounds__(kThreads) void logprob_join_k(const T *x, int64_t l
 // ---- gradient ------------------------------------------------------------------------------------------------
 
 // 2^tshift neighbouring threads share a row; blockIdx.x counts pieces of FLY vectors a thread, blockIdx.y groups of rows.
-template <typename T>
+template <typename T, bool ENTROPY>
 __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t rows, int64_t ld, int classes, int tshift,
                                                           const int64_t *labels, const float *lse, const float *entropy,
                                                           const float *d_logprob, const float *d_entropy, float scale, T *out,
@@ -575,25 +575,35 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
         T *to = out + at * out_ld;
         const int skew = skew_of(to, classes), vecs = (classes + skew + E - 1) / E;
         const int64_t label = labels ? labels[at] : RVN_NO_LABEL;
-        const float norm = lse[at];
-        float given = 0.f, spread = 0.f, h = 0.f;
-        if (label != RVN_NO_LABEL) given = label >= 0 && label < classes ? scale * (d_logprob ? d_logprob[at] : 1.f) : __uint_as_float(0x7fc00000u);
-        if (d_entropy) spread = scale * d_entropy[at], h = entropy[at];
-        // a term whose weight is 0 is absent, whatever the row holds; so is every term of a row that has no class
-        const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
+        // a row of no weight is not read where that shows before its other scalars have come
+        const bool idle = !ENTROPY && label == RVN_NO_LABEL;
         float g[Vec<T>::FLY][E];
 #pragma unroll
         for (int u = 0; u < Vec<T>::FLY; ++u)
-            load_vec(row, (v0 + u * team) * E - skew, none ? 0 : classes, -reach(at, ld), classes + reach(rows - 1 - at, ld), g[u]);
+            load_vec(row, (v0 + u * team) * E - skew, idle ? 0 : classes, -reach(at, ld), classes + reach(rows - 1 - at, ld), g[u]);
+        const float norm = lse[at];
+        float given = 0.f, spread = 0.f, h = 0.f;
+        if (label != RVN_NO_LABEL) given = label >= 0 && label < classes ? scale * (d_logprob ? d_logprob[at] : 1.f) : __uint_as_float(0x7fc00000u);
+        if (ENTROPY) spread = scale * d_entropy[at], h = entropy[at];
+        // a term whose weight is 0 is absent, whatever the row holds; so is every term of a row that has no class
+        const bool none = (given == 0.f && spread == 0.f) || norm == -INFINITY;
 #pragma unroll
         for (int u = 0; u < Vec<T>::FLY; ++u) {
             const int first = (v0 + u * team) * E - skew;
+            if (none) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float logp = g[u][e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
-                float d = -given * p;
-                if (d_entropy) d -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
-                g[u][e] = none ? 0.f : label == first + e ? d + given : d;
+                for (int e = 0; e < E; ++e) g[u][e] = 0.f;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    const float logp = g[u][e] - norm, p = __builtin_amdgcn_exp2f(logp * kLog2e);
+                    g[u][e] = -given * p;
+                    if (ENTROPY) g[u][e] -= spread * (p * (fmaxf(logp, -200.f) + h));  // (p is 0 there)
+                }
+                if (label >= first && label < first + E) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) g[u][e] += label == first + e ? given : 0.f;
+                }
             }
             if (first >= 0 && first + E <= classes) {
                 *reinterpret_cast<u4 *>(to + first) = Vec<T>::narrow(g[u]);
@@ -661,7 +671,7 @@ void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse,
     while (tshift < 8 && (Vec<T>::FLY << tshift) < vecs) ++tshift;
     const int64_t groups = (x.rows + (kThreads >> tshift) - 1) / (kThreads >> tshift);
     const dim3 grid((unsigned)((vecs + (Vec<T>::FLY << tshift) - 1) / (Vec<T>::FLY << tshift)), (unsigned)(groups < 65535 ? groups : 65535));
-    cx.run(logprob_bwd_k<T>, grid, dim3(kThreads), 0, static_cast<const T *>(x.p), x.rows, x.ld, x.classes, tshift, labels, lse, entropy,
+    cx.run(d_entropy ? logprob_bwd_k<T, true> : logprob_bwd_k<T, false>, grid, dim3(kThreads), 0, static_cast<const T *>(x.p), x.rows, x.ld, x.classes, tshift, labels, lse, entropy,
            d_logprob, d_entropy, scale, out, out_ld);
 }
 
