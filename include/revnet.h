@@ -603,7 +603,7 @@ int revnet_head_bwd(const rvn_head_desc *desc, const rvn_tensor *x, const void *
 
 /*
  * Log probabilities of given labels (class or token numbers) under the softmax
- * of each row of `logits` (fp32 or bf16, [rows][classes], classes < 2^31), with
+ * of each row of `logits` (fp32 or bf16, [rows][classes]; up to 2^31-1 rows, 2^30 classes), with
  * the entropy of the row's distribution, the logarithm of its normaliser and
  * its most likely classes, in one pass over the logits:
  *     lse = log sum_j exp(x_j),  logprob = x_label - lse,

@@ -15,6 +15,8 @@
 // it has kept in registers, or by reading the thread's vectors again where a second group reaches the bound -- and each takes
 // the place that the number of larger keys in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
 // wavefront takes its largest keys one by one and the lists are merged.
+#include <algorithm>
+
 #include "kernels.h"
 #include "quads.h"
 
@@ -640,10 +642,12 @@ Shape shape_of(int64_t rows, int classes, int size, int top_k) {
     return Shape{false, (classes + share - 1) / share, share};
 }
 
+// A launch counts its threads in 32 bits: rows beyond these, at 256 threads each, take another.
+constexpr int64_t kRowsAtOnce = 1 << 23;
+
 template <typename T>
-void forward(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch) {
+void forward(Ctx &cx, const Logits &x, const Shape &s, const int64_t *labels, const LogprobOut &out, void *scratch) {
     const T *p = static_cast<const T *>(x.p);
-    const Shape s = shape_of(x.rows, x.classes, (int)sizeof(T), out.top_k);
     const double bytes = (double)x.rows * ((double)x.classes * sizeof(T) + 20.0 + 12.0 * out.top_k);
     if (!cx.launch(K_LOGPROB, bytes, 5.0 * (double)x.rows * x.classes)) return;
     if (s.wave) {
@@ -697,8 +701,17 @@ size_t logprob_scratch_bytes(int64_t rows, int classes, int top_k) {
 }
 
 void logprob_fwd(Ctx &cx, const Logits &x, const int64_t *labels, const LogprobOut &out, void *scratch) {
-    if (x.bf16) forward<Bf16>(cx, x, labels, out, scratch);
-    else forward<float>(cx, x, labels, out, scratch);
+    const int size = x.bf16 ? 2 : 4;
+    const Shape s = shape_of(x.rows, x.classes, size, out.top_k);
+    for (int64_t at = 0; at < x.rows; at += kRowsAtOnce) {
+        const int64_t k = at * out.top_k;
+        const Logits part{static_cast<const char *>(x.p) + at * x.ld * size, x.bf16, std::min(x.rows - at, kRowsAtOnce), x.ld, x.classes};
+        const LogprobOut to{out.logprob ? out.logprob + at : nullptr, out.entropy ? out.entropy + at : nullptr, out.lse ? out.lse + at : nullptr,
+                            out.top_ids ? out.top_ids + k : nullptr, out.top_logprob ? out.top_logprob + k : nullptr, out.top_k};
+        const int64_t *const given = labels ? labels + at : nullptr;
+        if (x.bf16) forward<Bf16>(cx, part, s, given, to, scratch);
+        else forward<float>(cx, part, s, given, to, scratch);
+    }
 }
 
 void logprob_bwd(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse, const float *entropy, const float *d_logprob,

@@ -287,3 +287,25 @@ def test_two_streams_and_a_graph():
             for name in ("logprob", "entropy", "lse", "ids", "top"):
                 assert torch.equal(getattr(o, name), getattr(c["o"], name)), name
             assert torch.equal(g, c["g"])
+
+
+def test_more_rows_than_one_launch_has_threads_for():
+    """2^26 + 5 rows, a wavefront each: the rows where one launch ends and the next begins, and the last."""
+    import torch
+    import paper_1707_04585_amd as rv
+    rows, classes, step = 2 ** 26 + 5, 3, 2 ** 23
+    t = torch.ones((rows, classes), dtype=torch.bfloat16, device="cuda")
+    some, x = logits(np.random.default_rng(8), 12, classes, True)
+    at = torch.as_tensor([0, 1, step - 2, step - 1, step, step + 1, 3 * step - 1, 3 * step, 8 * step - 1, 8 * step, rows - 2, rows - 1], device="cuda")
+    t[at] = some
+    lab = torch.arange(rows, device="cuda") % classes
+    out = forward(t, lab, 2)
+    part = at.cpu().numpy()
+    check({k: v[part] for k, v in out.host().items()}, R.logprob(x, lab[at].cpu().numpy(), 2))
+    flat = R.logprob(np.ones((1, classes)), np.zeros(1, np.int64), 2)
+    rest = torch.ones(rows, dtype=torch.bool, device="cuda")
+    rest[at] = False
+    for name, bar in (("lse", flat["tol"][0]), ("logprob", flat["tol"][0] + 4 * R.EPS * np.log(3)), ("entropy", flat["tol_entropy"][0])):
+        got = getattr(out, name)[rest].double()
+        assert float((got - float(flat[name][0])).abs().max()) <= float(bar), name
+    assert int((out.ids[rest] != torch.tensor([0, 1], device="cuda")).sum()) == 0
