@@ -477,7 +477,10 @@ int revnet_stack_bwd_fixed(const rvn_block_desc *desc, int32_t depth, int32_t fr
  * Memory: codes [n][c][h*w] (int8, dense), zero to 255 unused bytes up to the
  * next multiple of 256, scales [n][c][ceil(h*w / RVN_CKPT_GROUP)] (fp32, dense).
  * ckpt: device, 256-byte aligned, at least revnet_ckpt_bytes of it, which must
- * not overlap a tensor of the same call.  Errors as for the other entry points.
+ * not overlap a tensor of the same call.  Sizes: as for the other entry points,
+ * c up to 65535, c * ceil(h*w / 4) up to 2^30 and 2^33 over the n images (and
+ * of every layer's input, in a stack or body that stores).  Errors as for the
+ * other entry points.
  * ---------------------------------------------------------------------- */
 #define RVN_CKPT_GROUP 128
 int revnet_ckpt_bytes(int64_t n, int64_t c, int64_t h, int64_t w, size_t *bytes);
@@ -568,7 +571,8 @@ typedef struct {
 /*
  * Head: the network's last layers, after the body (the paper follows the
  * residual networks it cites): logits = fc(mean over pixels of ReLU(BN(x))).
- * x [n, c, h, w] is the last stage's top (n*h*w up to 2^31-1, n up to 65535);
+ * x [n, c, h, w] is the last stage's top (n*h*w up to 2^31-1, n up to 65535,
+ * n*c up to 2^30, c*classes up to 2^31-1, classes up to 2^20);
  * logits fp32 [n][classes].  `saved` is a buffer of the caller's (256-byte
  * aligned, saved_bytes) that carries the batch statistics and the pooled values
  * from revnet_head_fwd to revnet_head_bwd.  All arithmetic is fp32.

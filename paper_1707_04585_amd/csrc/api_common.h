@@ -38,6 +38,8 @@ int check_geo(int64_t n, int64_t h, int64_t w);
 int check_ws(const void *ws, size_t have, size_t need);
 // A buffer of the caller's that carries state from one call to another (checkpoint, store, what a head saves).
 int check_store(const char *name, const void *p, size_t have, size_t need);
+// Sizes that the checkpoint kernels can count: see revnet.h.
+int check_ckpt_extent(int64_t c, const Geo &g);
 bool ranges_overlap(const void *a, size_t a_bytes, const void *b, size_t b_bytes);
 int check_params(const rvn_block_desc &d, const rvn_block_params *p, const char *what);
 int check_grads(const rvn_block_desc &d, const rvn_block_grads *p, const char *what);
@@ -106,6 +108,7 @@ struct StorePlan {
     size_t func;                              // bytes of one function
     size_t stack(int depth) const { return 2 * func * (size_t)depth; }
 };
+int check_store_extent(const rvn_block_desc &d, const Geo &g);
 StorePlan make_store_plan(const rvn_block_desc &d, const Geo &g);
 // Checkpoint buffers as a caller sees them: codes, then scales from the next multiple of 256 bytes.
 inline size_t ckpt_codes_bytes(int c, const Geo &g) { return align_up((size_t)g.pixels() * (size_t)c); }

@@ -368,6 +368,12 @@ size_t body_store_at(const rvn_body_desc &bd, const Geo &g0, int stage) {
     return off;
 }
 
+int check_body_store(const rvn_body_desc &bd, const Geo &g0) {
+    for (int s = 0; s < bd.stages; ++s)
+        if (int rc = check_store_extent(bd.stage[s], Geo{g0.n, g0.h >> s, g0.w >> s})) return rc;
+    return RVN_OK;
+}
+
 size_t body_stored_bwd_bytes(const rvn_body_desc &bd, const Geo &g0) {
     size_t most = body_ws(bd, g0, true, false).total;
     for (int s = 0; s < bd.stages; ++s) {
@@ -501,6 +507,7 @@ int body_fwd_impl(const rvn_body_desc *desc, const rvn_tensor *x, const rvn_bloc
     for (int s = 0; s < bd.stages; ++s)
         if (overlaps_range(&tops[s], ws, need)) return fail(RVN_ERR_ALIAS, "tops[%d] overlaps the workspace", s);
     if (storing) {
+        if (int rc = check_body_store(bd, g0)) return rc;
         const size_t store_need = body_store_at(bd, g0, bd.stages);
         if (int rc = check_store("store", store, store_bytes, store_need)) return rc;
         if (ranges_overlap(store, store_need, ws, need)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
@@ -594,6 +601,7 @@ int body_bwd_impl(const rvn_body_desc *desc, const rvn_tensor *tops, const rvn_t
         if (overlaps_range(&tops[s], ws, need) || overlaps_range(&dtops[s], ws, need))
             return fail(RVN_ERR_ALIAS, "tops[%d] or dtops[%d] overlaps the workspace", s, s);
     if (storing) {
+        if (int rc = check_body_store(bd, g0)) return rc;
         const size_t store_need = body_store_at(bd, g0, bd.stages);
         if (int rc = check_store("store", store, store_bytes, store_need)) return rc;
         if (ranges_overlap(store, store_need, ws, need)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
@@ -655,6 +663,7 @@ int revnet_body_stored_bytes(const rvn_body_desc *desc, int64_t n, int64_t h, in
                              size_t *bwd_ws_bytes) {
     if (int rc = check_body_desc(desc, n, h, w)) return rc;
     const Geo g{(int)n, (int)h, (int)w};
+    if (int rc = check_body_store(*desc, g)) return rc;
     if (store_bytes) *store_bytes = body_store_at(*desc, g, desc->stages);
     if (fwd_ws_bytes) *fwd_ws_bytes = body_ws_bytes(*desc, g, false);
     if (bwd_ws_bytes) *bwd_ws_bytes = body_stored_bwd_bytes(*desc, g);

@@ -240,8 +240,8 @@ __device__ __forceinline__ void put_quad(f4 r, QuadAt q, float *out, uint16_t *o
 
 constexpr int kFly = 4;  // quads a thread requests before it uses the first
 
-// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads (at most a few
-// hundred terms each) and wavefronts add in fp32, everything above in double
+// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads (52
+// terms at 256 x 64 x 56 x 56) and wavefronts add in fp32, everything above in double
 template <bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, int share,
                                                              double2 *sums) {
@@ -445,7 +445,8 @@ void ckpt_load(Ctx &cx, const CkptTensor *t, int count, Geo g, const PrepArgs *c
     if (!cx.launch(K_CKPT, bytes + carry_bytes)) return;
     PrepArgs prep{};
     if (carry) prep = *carry;
-    const int images = (int)std::max<int64_t>(1, std::min<int64_t>(g.n, (1 << 30) / blocks));
+    // (a launch counts its threads in 32 bits: the workgroups of at most 2^23 / blocks images, which go on to the others)
+    const int images = (int)std::max<int64_t>(1, std::min<int64_t>(g.n, (1 << 23) / blocks));
     const dim3 grid((unsigned)images * blocks + (unsigned)prep.blocks);
     const bool whole = hw % 4 == 0;
     cx.run(prep.blocks > 0 ? (whole ? ckpt_load_k<true, true> : ckpt_load_k<false, true>) : (whole ? ckpt_load_k<true, false> : ckpt_load_k<false, false>),

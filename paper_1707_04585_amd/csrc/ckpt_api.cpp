@@ -8,7 +8,8 @@ namespace {
 
 int check_ckpt_shape(int64_t n, int64_t c, int64_t h, int64_t w) {
     if (c <= 0 || c > 65535) return fail(RVN_ERR_SHAPE, "c = %lld out of range [1, 65535]", (long long)c);
-    return check_geo(n, h, w);
+    if (int rc = check_geo(n, h, w)) return rc;
+    return check_ckpt_extent(c, Geo{(int)n, (int)h, (int)w});
 }
 
 Ckpt ckpt_of(void *p, int c, const Geo &g) {

@@ -33,6 +33,9 @@ int check_head(const rvn_head_desc *d, int64_t n, int64_t h, int64_t w) {
     if (!(d->bn_eps > 0.f)) return fail(RVN_ERR_SHAPE, "bn_eps must be > 0");
     if (int rc = check_geo(n, h, w)) return rc;
     if (n > 65535) return fail(RVN_ERR_SHAPE, "n = %lld exceeds 65535", (long long)n);
+    // (what the launches can count in tiles of 16 x 16, up to 512 threads each)
+    if (n * d->c > (1LL << 30) || (int64_t)d->c * d->classes > 0x7fffffffLL)
+        return fail(RVN_ERR_SHAPE, "n*c = %lld exceeds 2^30 or c*classes = %lld exceeds 2^31-1", (long long)(n * d->c), (long long)d->c * d->classes);
     return RVN_OK;
 }
 

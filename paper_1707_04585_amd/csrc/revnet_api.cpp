@@ -204,6 +204,14 @@ StorePlan make_store_plan(const rvn_block_desc &d, const Geo &g) {
     return s;
 }
 
+int check_store_extent(const rvn_block_desc &d, const Geo &g) {
+    Layer ly[3];
+    const int L = func_layers(d, ly);
+    for (int l = 0; l < L; ++l)
+        if (int rc = check_ckpt_extent(ly[l].cin, g)) return rc;
+    return RVN_OK;
+}
+
 StoredWs stored_bwd_ws(const Plan &p, const Geo &g) {
     size_t sums = 0;
     for (int l = 0; l < p.L; ++l) sums = std::max(sums, ckpt_bn_scratch_floats(p.layers[l].cin, g));
@@ -320,6 +328,13 @@ int check_store(const char *name, const void *p, size_t have, size_t need) {
     if (!p) return fail(RVN_ERR_NULL, "%s is NULL (%zu bytes needed)", name, need);
     if (reinterpret_cast<uintptr_t>(p) % kAlign) return fail(RVN_ERR_STRIDE, "%s is not %zu-byte aligned", name, kAlign);
     if (have < need) return fail(RVN_ERR_SHAPE, "%s has %zu bytes, %zu needed", name, have, need);
+    return RVN_OK;
+}
+
+int check_ckpt_extent(int64_t c, const Geo &g) {
+    const int64_t quads = (g.hw() + 3) / 4;
+    if (c * quads > (1LL << 30) || g.n * c * quads > (1LL << 33))
+        return fail(RVN_ERR_SHAPE, "c * ceil(h*w / 4) = %lld for %d images exceeds 2^30, or 2^33 in all", (long long)(c * quads), g.n);
     return RVN_OK;
 }
 
@@ -809,6 +824,7 @@ int revnet_stack_stored_bytes(const rvn_block_desc *desc, int32_t depth, int64_t
     if (int rc = check_geo(n, h, w)) return rc;
     if (depth <= 0) return fail(RVN_ERR_SHAPE, "depth = %d must be positive", depth);
     const Geo g{(int)n, (int)h, (int)w};
+    if (int rc = check_store_extent(*desc, g)) return rc;
     if (store_bytes) *store_bytes = make_store_plan(*desc, g).stack(depth);
     if (fwd_ws_bytes) *fwd_ws_bytes = make_plan(*desc, g, false).total;
     if (bwd_ws_bytes) *bwd_ws_bytes = stored_bwd_ws(make_plan(*desc, g, true), g).total;
@@ -825,6 +841,7 @@ int revnet_stack_fwd_stored(const rvn_block_desc *desc, int32_t depth, const rvn
     if (!params) return fail(RVN_ERR_NULL, "params is NULL");
     for (int k = 0; k < depth; ++k)
         if (int rc = check_params(*desc, &params[k], "params")) return rc;
+    if (int rc = check_store_extent(*desc, g)) return rc;
     const size_t need = make_store_plan(*desc, g).stack(depth);
     if (int rc = check_store("store", store, store_bytes, need)) return rc;
     if (ranges_overlap(store, need, ws, pl.total)) return fail(RVN_ERR_ALIAS, "store overlaps the workspace");
@@ -860,6 +877,7 @@ int revnet_stack_bwd_stored(const rvn_block_desc *desc, int32_t depth, const rvn
         if (int rc = check_grads(*desc, &grads[k], "grads")) return rc;
     }
     const Geo g{(int)dy1->n, (int)dy1->h, (int)dy1->w};
+    if (int rc = check_store_extent(*desc, g)) return rc;
     const Plan pl = make_plan(*desc, g, true);
     const size_t ws_need = stored_bwd_ws(pl, g).total, need = make_store_plan(*desc, g).stack(depth);
     if (int rc = check_ws(ws, ws_bytes, ws_need)) return rc;

@@ -240,3 +240,21 @@ def test_on_another_stream_and_in_a_graph():
                 assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
             else:
                 assert torch.equal(own[name], eager[name]), name
+
+
+def test_more_planes_than_one_launch_has_threads_for():
+    """4.3e9 planes of one pixel, each a group of its own: off by the rounding of x / 126 and of 126 times that."""
+    import torch
+    import paper_1707_04585_amd as rv
+    n, c = 65600, 65535
+    a = torch.arange(n, device="cuda").float() % 251 - 125
+    b = torch.arange(c, device="cuda").float() % 509 * 0.25 - 60
+    x = torch.add(a[:, None], b[None, :]).view(n, c, 1, 1)
+    buf = torch.empty(rv.revnet_ckpt_bytes(n, c, 1, 1), dtype=torch.uint8, device="cuda")
+    rv.revnet_ckpt_save(x, None, buf)
+    x.fill_(9.0)
+    rv.revnet_ckpt_load(buf, x)
+    del buf
+    for i in range(0, n, 8200):
+        want = a[i:i + 8200, None] + b[None, :]
+        assert bool(((x[i:i + 8200, :, 0, 0] - want).abs() <= 3 * 2.0 ** -24 * want.abs()).all()), i

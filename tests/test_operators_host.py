@@ -274,3 +274,21 @@ def test_reference_codes_keep_the_decisions_and_stay_within_a_scale(h, w):
         assert np.all(np.abs(v.astype(np.float64) - x) <= steps * each * (1 + 1e-4))
         assert np.abs(q.astype(int)).max() <= (126 if st is None else 127)
     assert np.array_equal(R.positive(v, stats), R.positive(x, stats))
+
+
+def test_sizes_that_the_launches_cannot_count_are_refused():
+    assert rv.revnet_ckpt_bytes(1, 64, 8192, 8192) > 0                               # 2^30 quads, the most
+    assert status_of(rv.revnet_ckpt_bytes, 1, 65, 8192, 8192)[0] == SHAPE
+    assert status_of(rv.revnet_ckpt_bn_relu_workspace_bytes, 1, 65, 8192, 8192)[0] == SHAPE
+    assert rv.revnet_ckpt_bytes(1 << 18, 32768, 1, 1) > 0                            # 2^33 in all
+    assert status_of(rv.revnet_ckpt_bytes, (1 << 18) + 1, 32768, 1, 1)[0] == SHAPE
+    big = fake(BASE, n=1, c=65, h=8192, w=8192)
+    assert status_of(rv.revnet_ckpt_save, big, None, (FAR, 1 << 50))[0] == SHAPE
+    assert status_of(rv.revnet_ckpt_load, (FAR, 1 << 50), big)[0] == SHAPE
+    assert rv.revnet_stack_stored_bytes(rv.BlockDesc("basic", 64), 1, 1, 8192, 8192)[0] > 0
+    assert status_of(rv.revnet_stack_stored_bytes, rv.BlockDesc("basic", 65), 1, 1, 8192, 8192)[0] == SHAPE
+    body = rv.BodyDesc([rv.BlockDesc("basic", 65), rv.BlockDesc("basic", 8)], [2, 3], [rv.DownDesc("basic", 130, 16)])
+    assert status_of(rv.revnet_body_stored_bytes, body, 1, 8192, 8192)[0] == SHAPE
+    assert rv.revnet_head_workspace_bytes(rv.HeadDesc(16384, 5), 65535, 1, 1)[0] > 0
+    assert status_of(rv.revnet_head_workspace_bytes, rv.HeadDesc(16385, 5), 65535, 1, 1)[0] == SHAPE
+    assert status_of(rv.revnet_head_workspace_bytes, rv.HeadDesc(2048, 1 << 20), 1, 1, 1)[0] == SHAPE
