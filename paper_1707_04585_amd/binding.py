@@ -294,9 +294,15 @@ _pack_tensor = struct.Struct("9q").pack
 _pack_matrix = struct.Struct("qi4x3q").pack
 
 
+def _float32(t):
+    if not isinstance(t, rvn_tensor) and _dtype_name(t.dtype) != "float32":
+        raise ValueError(f"tensors here are float32, not {_dtype_name(t.dtype)}")
+
+
 def _tensor_arg(t):
     if t is None or isinstance(t, rvn_tensor):
         return None if t is None else C.byref(t)
+    _float32(t)
     return _pack_tensor(t.data_ptr(), *t.shape, *t.stride())
 
 
@@ -624,9 +630,9 @@ def revnet_stack_fwd_stored(desc, depth, x1, x2, params, y1, y2, store, ws, stre
     p = pack_params(params)
     sp, sb = _ws(store)
     wp, wb = _ws(ws)
-    t = [_tensor(v) for v in (x1, x2, y1, y2)]
-    _check(load_library().revnet_stack_fwd_stored(C.byref(d), C.c_int32(depth), C.byref(t[0]), C.byref(t[1]), p, C.byref(t[2]),
-                                                  C.byref(t[3]), C.c_void_p(sp), C.c_size_t(sb), C.c_void_p(wp), C.c_size_t(wb),
+    t = [_tensor_arg(v) for v in (x1, x2, y1, y2)]
+    _check(load_library().revnet_stack_fwd_stored(C.byref(d), C.c_int32(depth), t[0], t[1], p, t[2], t[3],
+                                                  C.c_void_p(sp), C.c_size_t(sb), C.c_void_p(wp), C.c_size_t(wb),
                                                   C.c_void_p(_stream(stream))))
 
 
@@ -635,9 +641,9 @@ def revnet_stack_bwd_stored(desc, depth, dy1, dy2, params, dx1, dx2, grads, accu
     p, g = pack_params(params), pack_grads(grads)
     sp, sb = _ws(store)
     wp, wb = _ws(ws)
-    t = [_tensor(v) for v in (dy1, dy2, dx1, dx2)]
-    _check(load_library().revnet_stack_bwd_stored(C.byref(d), C.c_int32(depth), C.byref(t[0]), C.byref(t[1]), p, C.byref(t[2]),
-                                                  C.byref(t[3]), g, C.c_int(int(accumulate_wgrads)), C.c_void_p(sp), C.c_size_t(sb),
+    t = [_tensor_arg(v) for v in (dy1, dy2, dx1, dx2)]
+    _check(load_library().revnet_stack_bwd_stored(C.byref(d), C.c_int32(depth), t[0], t[1], p, t[2], t[3], g,
+                                                  C.c_int(int(accumulate_wgrads)), C.c_void_p(sp), C.c_size_t(sb),
                                                   C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))
 
 
@@ -655,8 +661,10 @@ def revnet_body_fwd_stored(desc, x, stage_params, down_params, tops, store, ws, 
     dp = pack_down(down_params)
     kp, kb = _ws(store)
     wp, wb = _ws(ws)
-    tx, tt = _tensor(x), _tensor_array(tops)
-    _check(load_library().revnet_body_fwd_stored(C.byref(d), C.byref(tx), sp, dp, tt, C.c_void_p(kp), C.c_size_t(kb), C.c_void_p(wp),
+    for v in tops:
+        _float32(v)
+    tt = _tensor_array(tops)
+    _check(load_library().revnet_body_fwd_stored(C.byref(d), _tensor_arg(x), sp, dp, tt, C.c_void_p(kp), C.c_size_t(kb), C.c_void_p(wp),
                                                  C.c_size_t(wb), C.c_void_p(_stream(stream))))
     del keep
 
@@ -669,6 +677,8 @@ def revnet_body_bwd_stored(desc, tops, dtops, stage_params, down_params, stage_g
     dp, dg = pack_down(down_params), pack_down(down_grads)
     kp, kb = _ws(store)
     wp, wb = _ws(ws)
+    for v in (*tops, *dtops):
+        _float32(v)
     tt, td = _tensor_array(tops), _tensor_array(dtops)
     _check(load_library().revnet_body_bwd_stored(C.byref(d), tt, td, sp, dp, sg, dg, C.c_int(int(accumulate_wgrads)), C.c_void_p(kp),
                                                  C.c_size_t(kb), C.c_void_p(wp), C.c_size_t(wb), C.c_void_p(_stream(stream))))

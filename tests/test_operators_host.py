@@ -65,6 +65,15 @@ def test_arrays_of_the_wrong_type_or_length_are_refused_by_the_binding():
     for stats in (torch.zeros(4, 4, dtype=torch.float64), torch.zeros(4, 3), torch.zeros(4, 8)[:, ::2]):
         with pytest.raises(ValueError):
             rv.revnet_ckpt_save(x, stats, k)
+    for dtype in (torch.bfloat16, torch.float64, torch.int32):
+        y = torch.zeros(2, 4, 4, 4, dtype=dtype)
+        for call in (lambda: rv.revnet_ckpt_save(y, None, k), lambda: rv.revnet_ckpt_load(k, y),
+                     lambda: rv.revnet_body_fwd_stored(rv.BodyDesc([rv.BlockDesc("basic", 4)], [1], []), x, [[fake_params(rv.BlockDesc("basic", 4))]], [], [y], k, k),
+                     lambda: rv.revnet_stack_fwd_stored(rv.BlockDesc("basic", 4), 1, x, y, [fake_params(rv.BlockDesc("basic", 4))], x, x, k, k),
+                     lambda: rv.revnet_stack_bwd_stored(rv.BlockDesc("basic", 4), 1, x, x, [fake_params(rv.BlockDesc("basic", 4))], y, x,
+                                                        [fake_params(rv.BlockDesc("basic", 4))], 0, k, k)):
+            with pytest.raises(ValueError):
+                call()
     logits, out = torch.zeros(3, 5), torch.zeros(3)
     for labels in (torch.zeros(3, dtype=torch.int32), torch.zeros(2, dtype=torch.int64), torch.zeros(6, dtype=torch.int64)[::2]):
         with pytest.raises(ValueError):
