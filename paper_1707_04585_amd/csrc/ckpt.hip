@@ -357,7 +357,7 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
         }
     }
     __shared__ double part[T / 64][2];
-    const int ch = (int)blockIdx.x - carry.blocks, total = b.N * (int)b.by_per.d;
+    const int ch = channel_of((int)blockIdx.x - carry.blocks, b.C), total = b.N * (int)b.by_per.d;
     const Channel c = channel(b, ch);
     f4 dz[kFusedQuads], xm[kFusedQuads];
     float a0 = 0.f, a1 = 0.f;

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
                                                   float *__restrict__ stats, float *__restrict__ pooled, float *__restrict__ count,
                                                   float *__restrict__ xhat) {
     __shared__ float lds[TH / 64][3];
-    const int ch = (int)blockIdx.x, wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+    const int ch = channel_of((int)blockIdx.x, g.C), wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
     const int T = 1 << g.tshift, sub = lane & (T - 1), planes = 64 >> g.tshift;
     const float *base = x + (int64_t)ch * sc;
     f4 held[HELD > 0 ? HELD : 1];
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__r
                                                                 const float *__restrict__ d_pooled, float *dgamma, float *dbeta,
                                                                 int accumulate, float *__restrict__ dx, int64_t osn, int64_t osc) {
     __shared__ double lds[2][kPoolThreads / 64];
-    const int ch = (int)blockIdx.y, per = (int)by_per.d, total = N * per;
+    const int ch = channel_of((int)blockIdx.y, C), per = (int)by_per.d, total = N * per;
     const float mean = stats[ch], rstd = stats[C + ch], scale = stats[2 * C + ch], shift = stats[3 * C + ch];
     const float inv_hw = 1.f / (float)HW;
     const float *g = d_pooled + (int64_t)ch * N, *cnt = count + (int64_t)ch * N, *hat = xhat + (int64_t)ch * N;
