@@ -327,8 +327,8 @@ __global__ __launch_bounds__(kBackwardWaves * 64, 4) void head_linear_bwd_k(cons
     __shared__ TileLds<kBackwardWaves> lds;
     const int tiles_c = (c + 15) / 16;
     if ((int)blockIdx.x < data_blocks) {
-        const int tm = (int)blockIdx.x / tiles_c, tc = (int)blockIdx.x - tm * tiles_c;
-        tile<4, true, false>(dl, ld, n, tm * 16, w, c, c, tc * 16, classes, lds,
+        const int tm = (int)blockIdx.x / tiles_c, tc = channel_of((int)blockIdx.x - tm * tiles_c, tiles_c);
+        tile<8, true, false>(dl, ld, n, tm * 16, w, c, c, tc * 16, classes, lds,
                           [&](int i, int ch, float v) { d_pooled[(int64_t)ch * n + i] = v; }, [](int, float) {});
         return;
     }
