@@ -305,6 +305,7 @@ __device__ __forceinline__ void list_top(const Part<T> &p, int thread, const Top
     team_barrier<NW>();
     uint32_t bound = 0;
     for (int bit = 31; bit >= 16; --bit) {
+        if (bit == 31 && min(p.vecs, p.NT) <= top_k) break;  // no more threads than that have a vector: all is listed
         const uint32_t next = bound | 1u << bit;
         int count = 0;
 #pragma unroll
