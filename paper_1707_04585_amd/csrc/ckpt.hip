@@ -35,7 +35,8 @@ __device__ __forceinline__ uint32_t load_codes(const int8_t *plane, QuadAt q) {
     for (int j = 0; j < 3; ++j) v |= j < q.end ? (uint32_t)(uint8_t)plane[j] << (8 * j) : 0u;
     return v;
 }
-// FAR: nothing reads the codes soon, they shall not push what the caches hold out of them
+// FAR: nothing reads the codes soon, they shall not push what the caches hold out of them (a stack of 12 bottleneck blocks that
+// stores, forward: 4.52 ms, 4.67 without)
 template <bool WHOLE, bool FAR>
 __device__ __forceinline__ void store_codes(int8_t *plane, QuadAt q, uint32_t word) {
     if (WHOLE || (q.from == 0 && q.end == 4)) {
@@ -471,8 +472,12 @@ void ckpt_bn_relu_bwd(Ctx &cx, Ckpt k, View da, int c, Geo g, const float *stats
     const View kv = skip ? *skip : View{nullptr, 0, 0};
     const int acc = accumulate ? 1 : 0;
     const double out_bytes = out16 ? 2.0 : skip ? 8.0 : 4.0;
+    // One launch where a workgroup of 256 threads holds a channel (32 x 512 x 7 x 7: 4.5 us, 8.5 in two passes; 32 x 16 x 14 x 14: 4.8
+    // and 5.9).  Of 1024 threads with up to four quads each always (64 x 16 x 14 x 14: 5.0 and 6.1; 64 x 256 x 14 x 14: 7.9 and 12.4), with up
+    // to eight from 64 channels on (150 x 64 x 14 x 14: 9.1 and 9.5; 150 x 16 x 14 x 14: 7.6 and 6.3, with most of the chip idle); these
+    // carry no other launch's work.
     const bool wide = total > kFusedQuads * kThreads, whole = hw % 4 == 0;
-    if (total <= kFusedQuads * 1024 && !(wide && (red.blocks > 0 || c < 256))) {
+    if (total <= kFusedQuads * 1024 && !(wide && (red.blocks > 0 || (total > 4096 && c < 64)))) {
         if (!cx.launch(K_BN_BWD_APPLY, (5.0 + out_bytes) * elems)) return;
         const dim3 grid((unsigned)(c + red.blocks));
 #define RVN_FUSED(T, K)                                                                                                          \

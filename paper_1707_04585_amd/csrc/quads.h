@@ -21,7 +21,8 @@ struct QuadAt {
     int i, from, end;
     __device__ __forceinline__ bool owns(int j) const { return j >= from && j < end; }
 };
-// Quad k of a plane of hw pixels; WHOLE: hw is a multiple of four.
+// Quad k of a plane of hw pixels; WHOLE: hw is a multiple of four, which no quad's end has to be looked at for (32 x 64 x 56 x 56:
+// saving a checkpoint 8.5 us, by the general path 11.2; BN backward from codes 17.0 and 18.7, at 128 x 16 x 8 x 8 5.1 and 7.0).
 template <bool WHOLE>
 __device__ __forceinline__ QuadAt quad_at(int k, int hw) {
     if (WHOLE) return QuadAt{4 * k, 0, 4};

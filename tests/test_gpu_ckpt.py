@@ -148,6 +148,9 @@ BWD_SHAPES = [s for s in SHAPES if s[0] * s[2] * s[3] >= 4] + [
     (30, 280, 28, 28),    # one launch, 1024 threads
     (6, 2100, 45, 45),    # two launches, one workgroup's sums a channel
     (300, 3, 1, 5),
+    (70, 6, 14, 14),      # one launch, 1024 threads, few channels
+    (150, 9, 14, 14),     # as long a channel as fits, too few of them: two launches
+    (150, 66, 14, 14),    # enough of them: one
 ]
 
 
