@@ -274,15 +274,15 @@ struct TileLds {
     float rows[WAVES * 16];
 };
 
-// The 16 x WIDE tile at (m0, n0) of the product of an M x K and a K x N operand, its K split over the wavefronts of the
+// The 16 x 16 tile at (m0, n0) of the product of an M x K and a K x N operand, its K split over the wavefronts of the
 // workgroup and added in their order; put(m, n, value) stores an element that exists, put_rows(m, value) the sum of row m of A.
-template <int kAhead, bool A_ALONG, bool B_ALONG, int WIDE = 16, typename Lds, typename Put, typename PutRows>
+template <int kAhead, bool A_ALONG, bool B_ALONG, typename Lds, typename Put, typename PutRows>
 __device__ __forceinline__ void tile(const float *a, int64_t lda, int M, int m0, const float *b, int64_t ldb, int N, int n0, int K,
                                      Lds &lds, Put put, PutRows put_rows) {
     const int wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63, waves = (int)blockDim.x >> 6;
     const int each = ((K + 15) / 16 + waves - 1) / waves * 16, k0 = wave * each, k1 = min(K, k0 + each);
     const Operand<A_ALONG> oa(a, lda, m0, M);                                   // (rows and columns beyond the edge are computed,
-    const Operand<B_ALONG> ob[1] = {Operand<B_ALONG>(b, ldb, n0, min(N, n0 + WIDE))};  //  not stored)
+    const Operand<B_ALONG> ob[1] = {Operand<B_ALONG>(b, ldb, n0, N)};  //  not stored)
     f4 sum[1] = {{0.f, 0.f, 0.f, 0.f}};
     float rows = 0.f;
     accumulate_product<kAhead>(oa, ob, k0, k1, lds.turn[wave], sum, &rows);
@@ -301,18 +301,17 @@ __device__ __forceinline__ void tile(const float *a, int64_t lda, int M, int m0,
         const int m = m0 + (row ? o - 256 : o / 16), n = n0 + o % 16;
         if (m >= M) continue;
         if (row) put_rows(m, t);
-        else if (n < N && o % 16 < WIDE) put(m, n, t);
+        else if (n < N) put(m, n, t);
     }
 }
 
 constexpr int kForwardWaves = 16, kBackwardWaves = 8;  // the most of a workgroup
 
-template <int WIDE>
 __global__ __launch_bounds__(kForwardWaves * 64) void head_linear_k(const float *__restrict__ pooled, int n, int c, int classes,
                                                                  const float *__restrict__ w, const float *__restrict__ b,
                                                                  float *__restrict__ logits, int64_t ld) {
     __shared__ TileLds<kForwardWaves> lds;
-    tile<8, false, true, WIDE>(pooled, n, n, (int)blockIdx.y * 16, w, c, classes, (int)blockIdx.x * WIDE, c, lds,
+    tile<8, false, true>(pooled, n, n, (int)blockIdx.y * 16, w, c, classes, (int)blockIdx.x * 16, c, lds,
                      [&](int i, int k, float v) { logits[(int64_t)i * ld + k] = v + b[k]; }, [](int, float) {});
 }
 
@@ -378,9 +377,11 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
     p.J = (p.per + (1 << p.tshift) - 1) >> p.tshift;
     const int at_once = 64 >> p.tshift;
     auto steps = [&](int waves) { return (g.n + waves * at_once - 1) / (waves * at_once); };
-    // As few wavefronts a channel as keep its quads in registers, eight a lane, and fill the chip with eight a SIMD.
+    // As few wavefronts a channel as keep its quads in registers, eight a lane, and fill the chip with eight a SIMD or have one step
+    // of planes each.  (Whole forward passes: 32 x 2048 x 7 x 7 with 4: 16.8 us, with 16: 31.9, with 1: 20.3; 128 x 112 x 8 x 8 with 16: 9.3,
+    // with 4: 11.4; 64 x 512 x 4 x 4 with 4, a step each: 7.5, with 16: 11.6.)
     int waves = 1;
-    while (waves < 16 && ((int64_t)c * waves < 8192 || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
+    while (waves < 16 && (((int64_t)c * waves < 8192 && steps(waves) > 1) || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
     p.steps = steps(waves);
     const int64_t held = (int64_t)p.steps * p.J;
     const bool whole = g.hw() % 4 == 0;
@@ -397,8 +398,7 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
 
 void head_linear(Ctx &cx, const float *pooled, int n, int c, int classes, const float *w, const float *b, float *logits, int64_t ld) {
     if (!cx.launch(K_HEAD, 4.0 * ((double)n * c + (double)classes * c + (double)n * classes), 2.0 * n * (double)c * classes)) return;
-    const int rows = (n + 15) / 16, wide = (classes + 15) / 16 * rows >= 256 ? 16 : 8;
-    cx.run(wide == 16 ? head_linear_k<16> : head_linear_k<8>, dim3((unsigned)((classes + wide - 1) / wide), (unsigned)rows),
+    cx.run(head_linear_k, dim3((unsigned)((classes + 15) / 16), (unsigned)((n + 15) / 16)),
            dim3((unsigned)(64 * waves_for(c, kForwardWaves))), 0, pooled, n, c, classes, w, b, logits, ld);
 }
 
@@ -407,7 +407,10 @@ void head_linear_bwd(Ctx &cx, const float *dl, int64_t ld, const float *pooled, 
     if (!cx.launch(K_HEAD, 4.0 * (2.0 * n * c + 2.0 * classes * (double)c + (double)n * classes), 4.0 * n * (double)c * classes)) return;
     const int tiles_c = (c + 15) / 16, tiles_k = (classes + 15) / 16, data_blocks = tiles_c * ((n + 15) / 16);
     const int strips = ((c + 63) / 64) * tiles_k;
-    const bool in_strips = strips >= 1024;  // a wavefront for every SIMD
+    // Strips read the derivatives a quarter as often, but each goes through all images: where there are strips enough.  (Whole
+    // backward passes, by strips and by tiles: 32 x 2048 x 7 x 7, 1000 classes, 2016 strips 17.6 and 36.9 us; 8 x 512, 1000 classes, 504
+    // strips 8.4 and 12.8; 128 x 512 21.9 and 22.1; 256 x 512 35.6 and 29.7; 32 x 256, 100 classes, 28 strips 7.7 and 6.2.)
+    const bool in_strips = strips >= 256 + n;
     const int waves = waves_for(in_strips ? classes : std::max(classes, n), kBackwardWaves);
     cx.run(in_strips ? head_linear_bwd_k<true> : head_linear_bwd_k<false>,
            dim3((unsigned)(data_blocks + (in_strips ? (strips + waves - 1) / waves : tiles_c * tiles_k))), dim3((unsigned)(64 * waves)), 0, dl, ld,
