@@ -629,15 +629,18 @@ struct Shape {
 // by wavefronts in bf16, 37.3 and 28.7 in fp32; 2048 x 15000 bf16 20.3 and 18.4; 3000 x 32003 bf16 47.4 both, without top
 // classes 42.1 and 44.9.)  The more top classes, the more of a wavefront's 64 threads have to read their vectors again, which a
 // workgroup spreads over 256: 16 of 2048 x 15000 cost 21.9 and 22.4, 32 of them 24.2 and 31.8.
-// Else a row goes to a workgroup, or to several where there are fewer rows than compute units and each still has 16 KB to read.
+// Else a row goes to a workgroup, or to several, joined by a second launch, where the workgroups are few.  A second launch pays from
+// 56 KB a row on (5 top classes of 8 bf16 rows: 25000 classes 8.5 us in one launch, 9.6 in two; 40000 9.7 and 9.1).  The parts are
+// of 8 KB at least (1 x 40000 5.0 us, with 16 KB 5.3), from 64 rows on of 16 (100 x 50000, 5 top classes: 12.2, with 8 KB 13.1), from
+// 192 on, where rows alone nearly fill the chip, of 64 (300 x 131072: 18.6 us, 25.8 unsplit; 256 x 50021 with 5 top classes: 15.0
+// unsplit, 16.3 split).
 Shape shape_of(int64_t rows, int classes, int size, int top_k) {
     const int64_t bytes = (int64_t)classes * size;
     if (bytes <= 8192 || (rows >= 2048 && bytes <= 32768 && top_k <= 12)) return Shape{true, 1, classes};
-    if (rows >= 256) return Shape{false, 1, classes};
-    int64_t splits = (512 + rows - 1) / rows;
-    const int64_t most = (bytes + 16383) / 16384;
-    splits = splits < most ? splits : most;
-    splits = splits < 64 ? splits : 64;
+    const int64_t part = rows < 64 ? 8192 : rows < 192 ? 16384 : 65536;
+    const int64_t most = bytes <= 57344 ? 1 : rows < 192 ? (bytes + part - 1) / part : bytes / part;
+    const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), 1200 / rows));
+    if (splits == 1) return Shape{false, 1, classes};
     const int step = 16 / size;
     const int share = (int)(((classes + splits - 1) / splits + step - 1) / step * step);
     return Shape{false, (classes + share - 1) / share, share};

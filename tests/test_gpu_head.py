@@ -9,6 +9,7 @@ pytestmark = pytest.mark.gpu
 SIZES = [  # n, c, h, w, classes
     (2, 3, 2, 2, 2), (1, 5, 4, 4, 1), (4, 16, 8, 8, 10), (17, 33, 7, 7, 21), (5, 8, 1, 5, 300), (128, 112, 8, 8, 10), (32, 130, 7, 7, 1000),
     (3, 70, 15, 17, 33), (200, 20, 3, 3, 40), (6, 9, 56, 56, 12), (70, 12, 32, 32, 5), (33, 2050, 1, 1, 65), (2, 4, 90, 91, 7),
+    (8, 512, 3, 3, 1000), (37, 700, 2, 2, 610), (24, 2050, 7, 7, 501), (100, 2049, 7, 7, 3),
 ]
 BORDER = 1e-4
 

@@ -11,7 +11,7 @@ pytestmark = pytest.mark.gpu
 SIZES = [
     (1, 1, 1), (7, 2, 2), (5, 3, 0), (130, 10, 5), (3, 63, 32), (4, 64, 1), (6, 255, 32), (5, 256, 3), (33, 1000, 5), (2, 2047, 20),
     (3, 2048, 5), (3, 2049, 5), (9, 4095, 4), (3, 4097, 32), (300, 4111, 3), (260, 9001, 2), (1, 20011, 32), (5, 33000, 20), (40, 16400, 8),
-    (1, 131072, 32), (2, 262147, 5), (600, 2100, 1),
+    (1, 131072, 32), (2, 262147, 5), (600, 2100, 1), (193, 33001, 3), (70, 29001, 6),
 ]
 
 
