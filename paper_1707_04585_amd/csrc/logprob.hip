@@ -625,10 +625,11 @@ struct Shape {
 };
 
 // Rows up to 8 KB go to one wavefront each, and up to 32 KB where they are so many that each SIMD has two: a wavefront needs
-// no barrier, where a workgroup waits for its slowest at every join.  (8192 x 4200, 5 top classes: 35.1 us by workgroups, 24.1
-// by wavefronts in bf16, 37.3 and 28.7 in fp32; 2048 x 15000 bf16 20.3 and 18.4; 3000 x 32003 bf16 47.4 both, without top
-// classes 42.1 and 44.9.)  The more top classes, the more of a wavefront's 64 threads have to read their vectors again, which a
-// workgroup spreads over 256: 16 of 2048 x 15000 cost 21.9 and 22.4, 32 of them 24.2 and 31.8.
+// no barrier, where a workgroup waits for its slowest at every join.  (5 top classes, by workgroups and by wavefronts: 8192 x 1000
+// bf16 28.3 and 14.1 us, 32 x 2000 5.7 and 6.5; 8192 x 4200 bf16 35.1 and 24.1, fp32 37.3 and 28.7; 2048 x 15000 bf16 20.3 and
+// 18.4; 3000 x 32003 bf16 47.4 both, without top classes 42.1 and 44.9.)  The more top classes, the more of a wavefront's 64
+// threads have to read their vectors again, which a workgroup spreads over 256: 16 of 2048 x 15000 cost 21.9 and 22.4, 32 of them
+// 24.2 and 31.8.
 // Else a row goes to a workgroup, or to several, joined by a second launch, where the workgroups are few.  A second launch pays from
 // 56 KB a row on (5 top classes of 8 bf16 rows: 25000 classes 8.5 us in one launch, 9.6 in two; 40000 9.7 and 9.1).  The parts are
 // of 8 KB at least (1 x 40000 5.0 us, with 16 KB 5.3), from 64 rows on of 16 (100 x 50000, 5 top classes: 12.2, with 8 KB 13.1), from
