@@ -575,7 +575,8 @@ typedef struct {
  * n*c up to 2^30, c*classes up to 2^31-1, classes up to 2^20);
  * logits fp32 [n][classes].  `saved` is a buffer of the caller's (256-byte
  * aligned, saved_bytes) that carries the batch statistics and the pooled values
- * from revnet_head_fwd to revnet_head_bwd.  All arithmetic is fp32.
+ * from revnet_head_fwd to revnet_head_bwd.  All arithmetic is fp32.  An infinity
+ * or a NaN in a channel makes all logits NaN, and that channel's dx.
  */
 typedef struct {
     int32_t c, classes;

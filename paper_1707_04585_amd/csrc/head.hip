@@ -116,7 +116,7 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             const float z = fmaf(v[e], scale, shift);
-            if (live && at.owns(e) && z > 0.f) {
+            if (live && at.owns(e) && !(z <= 0.f)) {  // (a NaN is passed on)
                 sum += z;
                 pos += 1.f;
                 hat += (v[e] - mean) * rstd;

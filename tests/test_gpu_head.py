@@ -140,6 +140,19 @@ def test_channels_that_are_constant_or_never_positive():
     assert k.g["gamma"][2] == 0 and k.g["beta"][2] == 0
 
 
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("n,c,h,w", [(4, 6, 5, 5), (20, 3, 8, 8), (70, 3, 32, 32)])
+def test_a_value_that_is_no_number_is_not_hidden(n, c, h, w, bad):
+    import torch
+    arrays = list(problem(np.random.default_rng(3), n, c, h, w, 9))
+    arrays[0][n - 2, 1, h - 1, w - 1] = bad
+    k = Head(n, c, h, w, 9, arrays)
+    k.step()
+    torch.cuda.synchronize()
+    assert torch.isnan(k.logits).all() and torch.isnan(k.dx[:, 1]).all() and torch.isnan(k.g["w"][:, 1]).all() and torch.isnan(k.g["gamma"][1])
+    assert torch.isfinite(k.dx[:, 0]).all() and torch.isfinite(k.g["w"][:, 0]).all() and torch.isfinite(k.g["gamma"][0])
+
+
 def test_graph():
     import torch
     rng = np.random.default_rng(2)
