@@ -100,11 +100,13 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, 
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 v[u][h] = f4{0.f, 0.f, 0.f, 0.f};
-                if (n0 + u < N && mine[h]) v[u][h] = load4<WHOLE>(px + (int64_t)(n0 + u) * sn, at[h]);
+                if (n0 + u < N && mine[h]) v[u][h] = fetch4<WHOLE>(px + (int64_t)(n0 + u) * sn, at[h]);
             }
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
             if (n0 + u >= N) break;  // (uniform)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) v[u][h] = own4<WHOLE>(v[u][h], at[h]);
             // magnitudes as bit patterns: these order as the values do, infinities and NaN on top
             uint32_t most = 0;
 #pragma unroll
@@ -206,16 +208,17 @@ __device__ __forceinline__ Quad fetch(const BnLayer &b, const Place &p, int ch, 
     if (live) {
         q.word = load_codes<WHOLE>(b.q + p.plane * b.HW, p.at);
         q.step = b.s[p.plane * b.G + p.k / (kCkptGroup / 4)];
-        q.da = load4<WHOLE>(da + (int64_t)p.n * dsn + (int64_t)ch * dsc, p.at);
+        q.da = fetch4<WHOLE>(da + (int64_t)p.n * dsn + (int64_t)ch * dsc, p.at);
     }
     return q;
 }
-// dz and x - mean (pixels that are not the quad's own: dz is zero, as their da is)
-__device__ __forceinline__ void quad(const Quad &q, const Channel &c, f4 &dz, f4 &xm) {
-    const f4 v = decode(q.word, q.step);
+// dz and x - mean (pixels that are not the quad's own: dz is zero)
+template <bool WHOLE>
+__device__ __forceinline__ void quad(const Quad &q, QuadAt at, const Channel &c, f4 &dz, f4 &xm) {
+    const f4 v = decode(q.word, q.step), da = own4<WHOLE>(q.da, at);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        dz[j] = fmaf(v[j], c.scale, c.shift) > 0.f ? q.da[j] : 0.f;
+        dz[j] = fmaf(v[j], c.scale, c.shift) > 0.f ? da[j] : 0.f;
         xm[j] = v[j] - c.mean;
     }
 }
@@ -261,7 +264,8 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, co
 #pragma unroll
         for (int u = 0; u < kFly; ++u) {
             f4 dz, xm;
-            quad(q[u], c, dz, xm);
+            const int e = e0 + u * kThreads;
+            quad<WHOLE>(q[u], place<WHOLE>(b, ch, e < last ? e : e0).at, c, dz, xm);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 a0 += dz[j];
@@ -320,7 +324,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
         const int e = e0 + u * kThreads;
         const Place p = place<WHOLE>(b, ch, e < total ? e : 0);
         q[u] = fetch<WHOLE>(b, p, ch, e < total, da, dsn, dsc);
-        if (SKIP && e < total) kv[u] = load4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
+        if (SKIP && e < total) kv[u] = fetch4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
     }
     // every wavefront adds the channel's partial sums for itself, in the same order
     const int lane = (int)threadIdx.x & 63;
@@ -335,7 +339,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
         if (e >= total) return;
         const Place p = place<WHOLE>(b, ch, e);
         f4 dz, xm;
-        quad(q[u], c, dz, xm);
+        quad<WHOLE>(q[u], p.at, c, dz, xm);
         f4 r = gradient(dz, xm, c, k);
         if (SKIP) r += kv[u];
         put_quad<WHOLE>(r, p.at, out + (int64_t)p.n * osn + (int64_t)ch * osc, out16 ? out16 + p.plane * b.HW : nullptr);
@@ -366,7 +370,8 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
     for (int u = 0; u < kFusedQuads; ++u) {
         if (u * T >= total) break;  // (uniform)
         const int e = (int)threadIdx.x + u * T;
-        quad(fetch<WHOLE>(b, place<WHOLE>(b, ch, e < total ? e : 0), ch, e < total, da, dsn, dsc), c, dz[u], xm[u]);
+        const Place p = place<WHOLE>(b, ch, e < total ? e : 0);
+        quad<WHOLE>(fetch<WHOLE>(b, p, ch, e < total, da, dsn, dsc), p.at, c, dz[u], xm[u]);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             a0 += dz[u][j];
@@ -387,7 +392,7 @@ __global__ __launch_bounds__(T) void ckpt_bn_fused_k(const BnLayer b, const floa
         if (e >= total) return;
         const Place p = place<WHOLE>(b, ch, e);
         f4 r = gradient(dz[u], xm[u], c, k);
-        if (SKIP) r += load4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
+        if (SKIP) r += fetch4<WHOLE>(skip + (int64_t)p.n * ksn + (int64_t)ch * ksc, p.at);
         put_quad<WHOLE>(r, p.at, out + (int64_t)p.n * osn + (int64_t)ch * osc, out16 ? out16 + p.plane * b.HW : nullptr);
     }
 }

@@ -61,7 +61,7 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
             const QuadAt at = quad_at<WHOLE>(quad, g.HW);
             f4 v = {0.f, 0.f, 0.f, 0.f};
             if (HELD > 0 && !first) v = held[k];
-            else if (live) v = load4<WHOLE>(base + (int64_t)n * sn, at);
+            else if (live) v = own4<WHOLE>(fetch4<WHOLE>(base + (int64_t)n * sn, at), at);
             if (HELD > 0 && first) held[k] = v;
             visit(v, n, at, live, j == g.J - 1);
             if (++j == g.J) j = 0, ++step;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(kPoolThreads) void head_pool_bwd_k(const float *__r
     for (int e = (int)blockIdx.x * share + (int)threadIdx.x; e < last; e += kPoolThreads) {
         const int n = quotient(e, by_per);
         const QuadAt at = quad_at<WHOLE>(e - n * per, HW);
-        const f4 v = load4<WHOLE>(x + (int64_t)n * sn + (int64_t)ch * sc, at);
+        const f4 v = fetch4<WHOLE>(x + (int64_t)n * sn + (int64_t)ch * sc, at);
         const float gn = g[n] * inv_hw;
         f4 r;
 #pragma unroll

@@ -30,21 +30,24 @@ __device__ __forceinline__ QuadAt quad_at(int k, int hw) {
     return QuadAt{i, 4 * k - i, min(4, hw - i)};
 }
 
-// (pixels that are not the quad's own read as zero and are not written)
+// The four pixels at a quad's place; those that are not its own are dropped afterwards (own4), so that no request waits for
+// the values of another.
 template <bool WHOLE>
-__device__ __forceinline__ f4 load4(const float *plane, QuadAt q) {
-    if (WHOLE) return *reinterpret_cast<const f4_any *>(plane + q.i);
-    f4 v = {0.f, 0.f, 0.f, 0.f};
-    if (q.end == 4) {
-        v = *reinterpret_cast<const f4_any *>(plane + q.i);
+__device__ __forceinline__ f4 fetch4(const float *plane, QuadAt q) {
+    if (WHOLE || q.end == 4) return *reinterpret_cast<const f4_any *>(plane + q.i);
+    f4 v = {0.f, 0.f, 0.f, 0.f};  // a plane of fewer than four pixels
 #pragma unroll
-        for (int j = 0; j < 3; ++j) v[j] = j < q.from ? 0.f : v[j];
-    } else {  // a plane of fewer than four pixels
-#pragma unroll
-        for (int j = 0; j < 3; ++j) v[j] = j < q.end ? plane[j] : 0.f;
-    }
+    for (int j = 0; j < 3; ++j) v[j] = j < q.end ? plane[j] : 0.f;
     return v;
 }
+template <bool WHOLE>
+__device__ __forceinline__ f4 own4(f4 v, QuadAt q) {
+    if (WHOLE) return v;
+#pragma unroll
+    for (int j = 0; j < 3; ++j) v[j] = j < q.from ? 0.f : v[j];
+    return v;
+}
+// (pixels that are not the quad's own are not written)
 template <bool WHOLE>
 __device__ __forceinline__ void store4(float *plane, QuadAt q, f4 v) {
     if (WHOLE || (q.from == 0 && q.end == 4)) {
