@@ -40,33 +40,52 @@ __device__ __forceinline__ double block_total(float v, double *lds) {
 }
 
 // HELD > 0: the channel stays in registers, steps * J <= HELD quads of it in each lane; otherwise it is read three times (the
-// second and third mostly from the caches).
-template <int TH, int HELD, bool WHOLE>
+// second and third mostly from the caches).  SINGLE: J == 1, a lane has the same quad of every plane of its.
+// With d = x - mean and the positive pixels of a plane (as z = x * scale + shift says, as in the backward pass), its sum of
+// ReLU(z) is scale * sum d + beta * count and that of xhat rstd * sum d: one sum and a count a pixel.  (Instructions of this kernel
+// took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel.)
+template <int TH, int HELD, bool WHOLE, bool SINGLE>
 __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, int64_t sn, int64_t sc, const Planes g, float eps,
                                                   const float *__restrict__ gamma, const float *__restrict__ beta,
                                                   float *__restrict__ stats, float *__restrict__ pooled, float *__restrict__ count,
                                                   float *__restrict__ xhat) {
     __shared__ float lds[TH / 64][3];
-    const int ch = channel_of((int)blockIdx.x, g.C), wave = (int)threadIdx.x >> 6, lane = (int)threadIdx.x & 63;
+    const int ch = channel_of((int)blockIdx.x, g.C), wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = (int)threadIdx.x & 63;
     const int T = 1 << g.tshift, sub = lane & (T - 1), planes = 64 >> g.tshift;
     const float *base = x + (int64_t)ch * sc;
+    const QuadAt only = quad_at<WHOLE>(sub, g.HW);
     f4 held[HELD > 0 ? HELD : 1];
-    // calls visit(value, plane, its quad, whether it exists, whether it is the plane's last) for every item of this lane, in
-    // order; a plane's items follow each other
+    // calls visit(value, whether each pixel is one of the item's own, plane, whether the item is the plane's last) for every item
+    // of this lane, in order; a plane's items follow each other
     auto each = [&](bool first, auto visit) {
         int step = 0, j = 0;
         auto item = [&](int k) {
-            const int n = (step * (TH / 64) + wave) * planes + (lane >> g.tshift), quad = j * T + sub;
+            const int n = (step * (TH / 64) + wave) * planes + (lane >> g.tshift), quad = SINGLE ? sub : j * T + sub;
             const bool live = n < g.N && quad < g.per;
-            const QuadAt at = quad_at<WHOLE>(quad, g.HW);
+            const QuadAt at = SINGLE ? only : quad_at<WHOLE>(quad, g.HW);
             f4 v = {0.f, 0.f, 0.f, 0.f};
             if (HELD > 0 && !first) v = held[k];
-            else if (live) v = own4<WHOLE>(fetch4<WHOLE>(base + (int64_t)n * sn, at), at);
+            else if (live) v = fetch4<WHOLE>(base + (int64_t)n * sn, at);
             if (HELD > 0 && first) held[k] = v;
-            visit(v, n, at, live, j == g.J - 1);
-            if (++j == g.J) j = 0, ++step;
+            bool own[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own[e] = live && (WHOLE || at.owns(e));
+            visit(v, own, n, SINGLE || j == g.J - 1);
+            if (SINGLE || ++j == g.J) j = 0, ++step;
         };
         if constexpr (HELD > 0) {
+            if (first) {  // (all requests before the first use)
+#pragma unroll
+                for (int k = 0; k < HELD; ++k) {
+                    if (step >= g.steps) break;
+                    const int n = (step * (TH / 64) + wave) * planes + (lane >> g.tshift), quad = SINGLE ? sub : j * T + sub;
+                    held[k] = f4{0.f, 0.f, 0.f, 0.f};
+                    if (n < g.N && quad < g.per) held[k] = fetch4<WHOLE>(base + (int64_t)n * sn, SINGLE ? only : quad_at<WHOLE>(quad, g.HW));
+                    if (SINGLE || ++j == g.J) j = 0, ++step;
+                }
+                step = j = 0;
+                first = false;
+            }
 #pragma unroll
             for (int k = 0; k < HELD; ++k)
                 if (step < g.steps) item(k);
@@ -75,17 +94,23 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
         }
     };
     // mean and squared deviations of every wavefront's pixels, joined over the workgroup in double
-    float sum = 0.f, pos = 0.f, hat = 0.f;
-    each(true, [&](f4 v, int, QuadAt at, bool live, bool) {
+    int mine = 0;  // planes of this wavefront
+    for (int s = 0; s < g.steps; ++s) mine += min(max(g.N - (s * (TH / 64) + wave) * planes, 0), planes);
+    const float here = (float)mine * (float)g.HW;
+    float sum = 0.f;
+    each(true, [&](f4 v, const bool (&own)[4], int, bool) {
+        if (!WHOLE) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = own[e] ? v[e] : 0.f;
+        }
         sum += (v.x + v.y) + (v.z + v.w);
-        if (live) pos += WHOLE ? 4.f : (float)(at.end - at.from);
     });
-    const float here = wave_total(pos), wave_mean = here > 0.f ? wave_total(sum) / here : 0.f;
+    const float wave_mean = mine > 0 ? wave_total(sum) / here : 0.f;
     sum = 0.f;
-    each(false, [&](f4 v, int, QuadAt at, bool live, bool) {
+    each(false, [&](f4 v, const bool (&own)[4], int, bool) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float d = live && at.owns(e) ? v[e] - wave_mean : 0.f;
+            const float d = own[e] ? v[e] - wave_mean : 0.f;
             sum = fmaf(d, d, sum);
         }
     });
@@ -102,8 +127,8 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
         const double d = lds[w][1] - mean_d;
         m2 += lds[w][2] + lds[w][0] * d * d;
     }
-    const float mean = (float)mean_d, rstd = 1.f / sqrtf((float)(m2 / m) + eps);
-    const float scale = gamma[ch] * rstd, shift = fmaf(-mean, scale, beta[ch]);
+    const float mean = (float)mean_d, rstd = 1.f / sqrtf((float)(m2 / m) + eps), center = beta[ch];
+    const float scale = gamma[ch] * rstd, shift = fmaf(-mean, scale, center);
     if (threadIdx.x == 0) {
         stats[ch] = mean;
         stats[g.C + ch] = rstd;
@@ -111,27 +136,24 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
         stats[3 * g.C + ch] = shift;
     }
     const float inv_hw = 1.f / (float)g.HW;
-    sum = pos = 0.f;
-    each(false, [&](f4 v, int n, QuadAt at, bool live, bool last) {
+    int pos = 0;
+    sum = 0.f;
+    each(false, [&](f4 v, const bool (&own)[4], int n, bool last) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float z = fmaf(v[e], scale, shift);
-            if (live && at.owns(e) && !(z <= 0.f)) {  // (a NaN is passed on)
-                sum += z;
-                pos += 1.f;
-                hat += (v[e] - mean) * rstd;
-            }
+            const bool positive = own[e] && !(fmaf(v[e], scale, shift) <= 0.f);  // (a NaN is passed on)
+            sum += positive ? v[e] - mean : 0.f;
+            pos += positive ? 1 : 0;
         }
         if (!last) return;
-        sum = team_total(sum, g.tshift);
-        pos = team_total(pos, g.tshift);
-        hat = team_total(hat, g.tshift);
+        const float d = team_total(sum, g.tshift), c = team_total((float)pos, g.tshift);
         if (sub == 0 && n < g.N) {
-            pooled[(int64_t)ch * g.N + n] = sum * inv_hw;
-            count[(int64_t)ch * g.N + n] = pos;
-            xhat[(int64_t)ch * g.N + n] = hat;
+            pooled[(int64_t)ch * g.N + n] = fmaf(scale, d, center * c) * inv_hw;
+            count[(int64_t)ch * g.N + n] = c;
+            xhat[(int64_t)ch * g.N + n] = rstd * d;
         }
-        sum = pos = hat = 0.f;
+        sum = 0.f;
+        pos = 0;
     });
 }
 
@@ -380,19 +402,21 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
     // As few wavefronts a channel as keep its quads in registers, eight a lane, and fill the chip with eight a SIMD or have one step
     // of planes each.  (Whole forward passes: 32 x 2048 x 7 x 7 with 4: 16.8 us, with 16: 31.9, with 1: 20.3; 128 x 112 x 8 x 8 with 16: 9.3,
     // with 4: 11.4; 64 x 512 x 4 x 4 with 4, a step each: 7.5, with 16: 11.6.)
-    int waves = 1;
+    int waves = p.J > 1 ? 16 : 1;
     while (waves < 16 && (((int64_t)c * waves < 8192 && steps(waves) > 1) || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
     p.steps = steps(waves);
     const int64_t held = (int64_t)p.steps * p.J;
     const bool whole = g.hw() % 4 == 0;
-#define RVN_POOL(TH, HELD)                                                                                                     \
-    cx.run(whole ? head_pool_k<TH, HELD, true> : head_pool_k<TH, HELD, false>, dim3((unsigned)c), dim3(TH), 0, x.p, x.sn, x.sc, p, eps, \
-           gamma, beta, s.stats, s.pooled, s.count, s.xhat)
-    if (held > 8) RVN_POOL(1024, 0);
-    else if (waves == 1) RVN_POOL(64, 8);
-    else if (waves == 4 && held > 2) RVN_POOL(256, 8);
-    else if (waves == 4) RVN_POOL(256, 2);
-    else RVN_POOL(1024, 8);
+#define RVN_POOL(TH, HELD, SINGLE)                                                                                                         \
+    cx.run(whole ? head_pool_k<TH, HELD, true, SINGLE> : head_pool_k<TH, HELD, false, SINGLE>, dim3((unsigned)c), dim3(TH), 0, x.p, x.sn, x.sc, p, \
+           eps, gamma, beta, s.stats, s.pooled, s.count, s.xhat)
+    if (held > 16) RVN_POOL(1024, 0, false);
+    else if (p.J > 1) RVN_POOL(1024, 16, false);
+    else if (held > 8) RVN_POOL(1024, 16, true);
+    else if (waves == 1) RVN_POOL(64, 8, true);
+    else if (waves == 4 && held > 2) RVN_POOL(256, 8, true);
+    else if (waves == 4) RVN_POOL(256, 2, true);
+    else RVN_POOL(1024, 8, true);
 #undef RVN_POOL
 }
 
