@@ -39,11 +39,12 @@ __device__ __forceinline__ double block_total(float v, double *lds) {
     return s;
 }
 
-// HELD > 0: the channel stays in registers, steps * J <= HELD quads of it in each lane; otherwise it is read three times (the
-// second and third mostly from the caches).  SINGLE: J == 1, a lane has the same quad of every plane of its.
+// HELD > 0: the channel stays in registers, steps * J <= HELD quads of it in each lane; otherwise it is read three times, the
+// second and third mostly from the caches (whole forward pass at 256 x 512 x 14 x 14 42.2 and 53.7 us).  SINGLE: J == 1, a lane has the
+// same quad of every plane of its (256 x 512 x 7 x 7: 27.1 and 30.8).
 // With d = x - mean and the positive pixels of a plane (as z = x * scale + shift says, as in the backward pass), its sum of
 // ReLU(z) is scale * sum d + beta * count and that of xhat rstd * sum d: one sum and a count a pixel.  (Instructions of this kernel
-// took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel.)
+// took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel; 21 us now.)
 template <int TH, int HELD, bool WHOLE, bool SINGLE>
 __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, int64_t sn, int64_t sc, const Planes g, float eps,
                                                   const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -146,7 +147,8 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
             pos += positive ? 1 : 0;
         }
         if (!last) return;
-        const float d = team_total(sum, g.tshift), c = team_total((float)pos, g.tshift);
+        float d = sum, c = (float)pos;
+        team_totals(d, c, g.tshift);
         if (sub == 0 && n < g.N) {
             pooled[(int64_t)ch * g.N + n] = fmaf(scale, d, center * c) * inv_hw;
             count[(int64_t)ch * g.N + n] = c;
@@ -400,8 +402,8 @@ void head_pool(Ctx &cx, View x, int c, Geo g, float eps, const float *gamma, con
     const int at_once = 64 >> p.tshift;
     auto steps = [&](int waves) { return (g.n + waves * at_once - 1) / (waves * at_once); };
     // As few wavefronts a channel as keep its quads in registers, eight a lane, and fill the chip with eight a SIMD or have one step
-    // of planes each.  (Whole forward passes: 32 x 2048 x 7 x 7 with 4: 16.8 us, with 16: 31.9, with 1: 20.3; 128 x 112 x 8 x 8 with 16: 9.3,
-    // with 4: 11.4; 64 x 512 x 4 x 4 with 4, a step each: 7.5, with 16: 11.6.)
+    // of planes each.  (Whole forward passes: 32 x 2048 x 7 x 7 with 4: 15.2 us, with 16: 31.2, with 1: 16.5; 32 x 256 x 7 x 7 with 16: 8.3,
+    // with 4: 10.0; 8 x 512 x 7 x 7 with 4, a step each: 7.1, with 16: 11.3.)
     int waves = p.J > 1 ? 16 : 1;
     while (waves < 16 && (((int64_t)c * waves < 8192 && steps(waves) > 1) || (int64_t)steps(waves) * p.J > 8)) waves *= 4;
     p.steps = steps(waves);

@@ -22,7 +22,7 @@ struct QuadAt {
     __device__ __forceinline__ bool owns(int j) const { return j >= from && j < end; }
 };
 // Quad k of a plane of hw pixels; WHOLE: hw is a multiple of four, which no quad's end has to be looked at for (32 x 64 x 56 x 56:
-// saving a checkpoint 8.5 us, by the general path 11.2; BN backward from codes 17.0 and 18.7, at 128 x 16 x 8 x 8 5.1 and 7.0).
+// saving a checkpoint 8.5 us, by the general path 10.6; BN backward from codes 17.1 and 17.8, at 128 x 16 x 8 x 8 5.1 and 6.8).
 template <bool WHOLE>
 __device__ __forceinline__ QuadAt quad_at(int k, int hw) {
     if (WHOLE) return QuadAt{4 * k, 0, 4};
@@ -88,17 +88,29 @@ __device__ __forceinline__ float wave_total(float v) {
 template <typename Combine>
 __device__ __forceinline__ uint32_t team_combine(uint32_t v, int shift, Combine combine) {
 #define RVN_MOVE(ctrl) (uint32_t) __builtin_amdgcn_update_dpp((int)v, (int)v, ctrl, 0xf, 0xf, true)
-    if (shift >= 1) v = combine(v, RVN_MOVE(0xb1));   // quad_perm 1 0 3 2
-    if (shift >= 2) v = combine(v, RVN_MOVE(0x4e));   // quad_perm 2 3 0 1
-    if (shift >= 3) v = combine(v, RVN_MOVE(0x141));  // row_half_mirror
-    if (shift >= 4) v = combine(v, RVN_MOVE(0x140));  // row_mirror
+    if (__builtin_expect(shift >= 1, 1)) v = combine(v, RVN_MOVE(0xb1));   // quad_perm 1 0 3 2
+    if (__builtin_expect(shift >= 2, 1)) v = combine(v, RVN_MOVE(0x4e));   // quad_perm 2 3 0 1
+    if (__builtin_expect(shift >= 3, 1)) v = combine(v, RVN_MOVE(0x141));  // row_half_mirror
+    if (__builtin_expect(shift >= 4, 1)) v = combine(v, RVN_MOVE(0x140));  // row_mirror
 #undef RVN_MOVE
     if (shift >= 5) v = combine(v, (uint32_t)__shfl_xor((int)v, 16, 64));
     if (shift >= 6) v = combine(v, (uint32_t)__shfl_xor((int)v, 32, 64));
     return v;
 }
-__device__ __forceinline__ float team_total(float v, int shift) {
-    return __uint_as_float(team_combine(__float_as_uint(v), shift, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+// Both values' sums over the team, in one walk through the steps, those of up to 16 lanes in line (the head's forward pass at
+// 256 x 512 x 14 x 14: 42.2 us, with two walks and jumps 49.6).
+__device__ __forceinline__ void team_totals(float &a, float &b, int shift) {
+    auto add = [](float v, uint32_t w) { return v + __uint_as_float(w); };
+#define RVN_MOVE(v, ctrl) (uint32_t) __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), ctrl, 0xf, 0xf, true)
+#define RVN_BOTH(ctrl) a = add(a, RVN_MOVE(a, ctrl)), b = add(b, RVN_MOVE(b, ctrl))
+    if (__builtin_expect(shift >= 1, 1)) RVN_BOTH(0xb1);
+    if (__builtin_expect(shift >= 2, 1)) RVN_BOTH(0x4e);
+    if (__builtin_expect(shift >= 3, 1)) RVN_BOTH(0x141);
+    if (__builtin_expect(shift >= 4, 1)) RVN_BOTH(0x140);
+#undef RVN_BOTH
+#undef RVN_MOVE
+    if (shift >= 5) a += __shfl_xor(a, 16, 64), b += __shfl_xor(b, 16, 64);
+    if (shift >= 6) a += __shfl_xor(a, 32, 64), b += __shfl_xor(b, 32, 64);
 }
 __device__ __forceinline__ uint32_t team_most(uint32_t v, int shift) {
     return team_combine(v, shift, [](uint32_t a, uint32_t b) { return max(a, b); });
