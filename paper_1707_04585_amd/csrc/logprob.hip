@@ -619,6 +619,8 @@ __global__ __launch_bounds__(kThreads) void logprob_bwd_k(const T *x, int64_t ro
     }
 }
 
+constexpr int kFewTop = 12;
+
 struct Shape {
     bool wave;           // a wavefront a row
     int splits, share;   // else workgroups a row, and the classes of each
@@ -632,13 +634,14 @@ struct Shape {
 // 24.2 and 31.8.
 // Else a row goes to a workgroup, or to several, joined by a second launch, where the workgroups are few.  A second launch pays from
 // 56 KB a row on (5 top classes of 8 bf16 rows: 25000 classes 8.5 us in one launch, 9.6 in two; 40000 9.7 and 9.1).  The parts are
-// of 8 KB at least (1 x 40000 5.0 us, with 16 KB 5.3), from 64 rows on of 16 (100 x 50000, 5 top classes: 12.2, with 8 KB 13.1), from
+// of 8 KB at least (1 x 40000 5.0 us, with 16 KB 5.3), with many top classes, of which each part lists so many, of 16 (1 x 65537 with
+// 20: 13.1 us, with 8 KB 14.2), as from 64 rows on (100 x 50000, 5 top classes: 12.2, with 8 KB 13.1), from
 // 192 on, where rows alone nearly fill the chip, of 64 (300 x 131072: 18.6 us, 25.8 unsplit; 256 x 50021 with 5 top classes: 15.0
 // unsplit, 16.3 split).
 Shape shape_of(int64_t rows, int classes, int size, int top_k) {
     const int64_t bytes = (int64_t)classes * size;
-    if (bytes <= 8192 || (rows >= 2048 && bytes <= 32768 && top_k <= 12)) return Shape{true, 1, classes};
-    const int64_t part = rows < 64 ? 8192 : rows < 192 ? 16384 : 65536;
+    if (bytes <= 8192 || (rows >= 2048 && bytes <= 32768 && top_k <= kFewTop)) return Shape{true, 1, classes};
+    const int64_t part = rows < 64 && top_k <= kFewTop ? 8192 : rows < 192 ? 16384 : 65536;
     const int64_t most = bytes <= 57344 ? 1 : rows < 192 ? (bytes + part - 1) / part : bytes / part;
     const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(most, 64), 1200 / rows));
     if (splits == 1) return Shape{false, 1, classes};
@@ -698,9 +701,11 @@ void backward(Ctx &cx, const Logits &x, const int64_t *labels, const float *lse,
 size_t logprob_scratch_bytes(int64_t rows, int classes, int top_k) {
     size_t most = 0;  // of the two types' shapes
     for (int size = 2; size <= 4; size += 2) {
-        const Shape s = shape_of(rows, classes, size, top_k);
-        const size_t need = s.splits > 1 ? (size_t)rows * s.splits * (sizeof(float4) + (size_t)top_k * sizeof(Key)) : 0;
-        most = most > need ? most : need;
+        for (int k : {top_k, std::min(top_k, kFewTop)}) {  // (enough for every smaller number of top classes, too)
+            const Shape s = shape_of(rows, classes, size, k);
+            const size_t need = s.splits > 1 ? (size_t)rows * s.splits * (sizeof(float4) + (size_t)k * sizeof(Key)) : 0;
+            most = most > need ? most : need;
+        }
     }
     return most;
 }

@@ -301,3 +301,9 @@ def test_sizes_that_the_launches_cannot_count_are_refused():
     assert rv.revnet_head_workspace_bytes(rv.HeadDesc(16384, 5), 65535, 1, 1)[0] > 0
     assert status_of(rv.revnet_head_workspace_bytes, rv.HeadDesc(16385, 5), 65535, 1, 1)[0] == SHAPE
     assert status_of(rv.revnet_head_workspace_bytes, rv.HeadDesc(2048, 1 << 20), 1, 1, 1)[0] == SHAPE
+
+
+@pytest.mark.parametrize("rows,classes", [(1, 65537), (3, 40000), (70, 131072), (300, 131072), (2048, 12000)])
+def test_log_probability_workspace_suffices_for_fewer_top_classes(rows, classes):
+    sizes = [rv.revnet_logprob_workspace_bytes(rows, classes, k) for k in range(rv.MAX_TOP_K + 1)]
+    assert sizes == sorted(sizes)
