@@ -73,7 +73,8 @@ __device__ __forceinline__ CkptTensor job_of(const Jobs &jobs, int &block) {
 
 // 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
 // pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
-// requests the quads of kFly images before it uses the first.
+// requests the quads of kFly images before it uses the first.  (64 x 128 x 56 x 56, half the channels of a tensor: 129 MB in 30 us,
+// 4.3 TB/s, half of it read from HBM; 128 x 512 x 13 x 13, with partial words at both ends of a plane, 3.4 TB/s.)
 template <bool BN, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, int HW, int G, FastDiv by_g, int tshift) {
     int block = (int)blockIdx.x;
@@ -140,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, 
 }
 
 // One lane per four pixels; prep.blocks workgroups convert filters, then come by_blocks.d workgroups (the quads of an image)
-// for each of `images` images at a time.
+// for each of `images` images at a time.  (The same 129 MB in 20.5 us, 6.3 TB/s: what is written stays in the nearer caches.)
 template <bool WHOLE, bool PREP>
 __global__ __launch_bounds__(kThreads) void ckpt_load_k(const Jobs jobs, int N, int HW, int G, FastDiv by_per, FastDiv by_blocks, int images,
                                                         const PrepArgs prep) {
@@ -244,8 +245,8 @@ __device__ __forceinline__ void put_quad(f4 r, QuadAt q, float *out, uint16_t *o
 
 constexpr int kFly = 4;  // quads a thread requests before it uses the first
 
-// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads (52
-// terms at 256 x 64 x 56 x 56) and wavefronts add in fp32, everything above in double
+// sums[ch][split] = (sum dz, sum dz * (x - mean)) over a share of a channel's quads; threads (52 terms at 256 x 64 x 56 x 56) and
+// wavefronts add in fp32, everything above in double.  Bound by memory (64 x 128 x 56 x 56: 129 MB in 30.7 us, 4.2 TB/s).
 template <bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_reduce_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc, int share,
                                                              double2 *sums) {
@@ -302,6 +303,7 @@ __device__ __forceinline__ void put_sums(const Channel &c, double sum, double su
 }
 
 // The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
+// (64 x 128 x 56 x 56 with a skip tensor: 335 MB in 54 us, 6.2 TB/s, part of the second read of codes and da from the caches.)
 template <bool SKIP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc,
                                                             const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_c, int chunks,
@@ -346,7 +348,8 @@ __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, con
     }
 }
 
-// Both passes in one launch where a channel's quads fit the registers of one workgroup: codes and da are read once.
+// Both passes in one launch where a channel's quads fit the registers of one workgroup: codes and da are read once.  (128 x 512 x 10 x 12:
+// 71 MB in 15.9 us, 4.5 TB/s; 32 x 512 x 7 x 7, 7.3 MB, 5.1 us, bound by latency.)
 constexpr int kFusedQuads = 8;
 
 template <int T, bool SKIP, bool WHOLE>

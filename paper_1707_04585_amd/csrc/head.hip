@@ -44,7 +44,8 @@ __device__ __forceinline__ double block_total(float v, double *lds) {
 // same quad of every plane of its (256 x 512 x 7 x 7: 27.1 and 30.8).
 // With d = x - mean and the positive pixels of a plane (as z = x * scale + shift says, as in the backward pass), its sum of
 // ReLU(z) is scale * sum d + beta * count and that of xhat rstd * sum d: one sum and a count a pixel.  (Instructions of this kernel
-// took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel; 21 us now.)
+// took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel; the whole
+// forward pass took 41.6 us then, 35.0 now.  32 x 2048 x 7 x 7: 12.8 MB in 8.0 us.)
 template <int TH, int HELD, bool WHOLE, bool SINGLE>
 __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, int64_t sn, int64_t sc, const Planes g, float eps,
                                                   const float *__restrict__ gamma, const float *__restrict__ beta,
@@ -159,7 +160,8 @@ __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, i
     });
 }
 
-// dx of a share of a channel's quads; every workgroup forms the channel's two sums for itself.
+// dx of a share of a channel's quads; every workgroup forms the channel's two sums for itself.  Bound by memory and, small, by
+// latency (32 x 2048 x 7 x 7: 25.7 MB in 7.0 us, 3.7 TB/s).
 constexpr int kPoolThreads = 256;
 
 template <bool WHOLE>
@@ -331,6 +333,8 @@ __device__ __forceinline__ void tile(const float *a, int64_t lda, int M, int m0,
 
 constexpr int kForwardWaves = 16, kBackwardWaves = 8;  // the most of a workgroup
 
+// A 16 x 16 tile of the logits, its reduction over the channels split over the wavefronts (32 x 2048 x 1000: 7.5 us, bound by the
+// latency of the weights' loads; 131 MFLOP).
 __global__ __launch_bounds__(kForwardWaves * 64) void head_linear_k(const float *__restrict__ pooled, int n, int c, int classes,
                                                                  const float *__restrict__ w, const float *__restrict__ b,
                                                                  float *__restrict__ logits, int64_t ld) {
@@ -342,6 +346,7 @@ __global__ __launch_bounds__(kForwardWaves * 64) void head_linear_k(const float 
 // The first `data_blocks` workgroups: d_pooled as [c][n], a tile each.  The others: the weights' gradient and, where the
 // channels begin, the bias's -- STRIPS: 16 classes by 64 channels per wavefront, which reads the 16 classes' derivatives once
 // for four tiles; else, where that leaves most of the chip idle, a tile per workgroup with the images split over its wavefronts.
+// (32 x 2048 x 1000: 10.8 us for 17 MB and 262 MFLOP.)
 template <bool STRIPS>
 __global__ __launch_bounds__(kBackwardWaves * 64, 4) void head_linear_bwd_k(const float *__restrict__ dl, int64_t ld, const float *__restrict__ pooled,
                                                                      int n, int c, int classes, const float *__restrict__ w,
