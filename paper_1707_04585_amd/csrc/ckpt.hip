@@ -74,7 +74,7 @@ __device__ __forceinline__ CkptTensor job_of(const Jobs &jobs, int &block) {
 // 2^tshift neighbouring lanes share a group: 16 lanes with two quads each, 64 pixels apart, or, on planes of at most 64
 // pixels, as many as the plane has quads with one each.  blockIdx.x counts the groups of an image, blockIdx.y images; a lane
 // requests the quads of kFly images before it uses the first.  (64 x 128 x 56 x 56, half the channels of a tensor: 129 MB in 30 us,
-// 4.3 TB/s, half of it read from HBM; 128 x 512 x 13 x 13, with partial words at both ends of a plane, 3.4 TB/s.)
+// 4.3 TB/s, mostly of reads; 128 x 512 x 13 x 13, with partial words at both ends of a plane, 3.4 TB/s.)
 template <bool BN, bool WHOLE, bool FAR>
 __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, int HW, int G, FastDiv by_g, int tshift) {
     int block = (int)blockIdx.x;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kThreads) void ckpt_save_k(const Jobs jobs, int N, 
 }
 
 // One lane per four pixels; prep.blocks workgroups convert filters, then come by_blocks.d workgroups (the quads of an image)
-// for each of `images` images at a time.  (The same 129 MB in 20.5 us, 6.3 TB/s: what is written stays in the nearer caches.)
+// for each of `images` images at a time.  (The same 129 MB in 20.5 us, 6.3 TB/s, mostly of writes, which a fill reaches 6.8 with.)
 template <bool WHOLE, bool PREP>
 __global__ __launch_bounds__(kThreads) void ckpt_load_k(const Jobs jobs, int N, int HW, int G, FastDiv by_per, FastDiv by_blocks, int images,
                                                         const PrepArgs prep) {
@@ -303,7 +303,7 @@ __device__ __forceinline__ void put_sums(const Channel &c, double sum, double su
 }
 
 // The first carry.blocks workgroups sum a filter gradient's partial results; the others take `chunks` shares of every channel.
-// (64 x 128 x 56 x 56 with a skip tensor: 335 MB in 54 us, 6.2 TB/s, part of the second read of codes and da from the caches.)
+// (64 x 128 x 56 x 56 with a skip tensor: 335 MB in 54 us, 6.2 TB/s, part of the second read of codes and da from the Infinity Cache.)
 template <bool SKIP, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void ckpt_bn_apply_k(const BnLayer b, const float *da, int64_t dsn, int64_t dsc,
                                                             const double2 *__restrict__ sums, int S, double inv_m, FastDiv by_c, int chunks,

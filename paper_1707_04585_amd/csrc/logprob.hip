@@ -6,15 +6,15 @@
 // t = sum 2^((x-m) L) (x-m) L with L = log2(e), and rescales s and t when m grows; joining two such triples is the same
 // step, so that threads, wavefronts and workgroups of a row join theirs in a fixed order.  With the total
 //     lse = m + ln s,   logprob = (x_label - m) - ln s,   entropy = ln s - ln 2 * t / s.
-// The sums are fp32: at most a few hundred terms in a thread, then a tree.
+// The sums are fp32: 512 terms in a thread at 131072 classes, then a tree.
 //
 // Top classes.  Classes are ordered by one 64-bit key: the value's bits made monotonic, above the complement of the class
 // number, so that no two are equal.  Every thread of a row knows the largest value of its own vectors; the top_k-th largest
 // of these (to 16 bits, by bisection: count the threads at or above a bit pattern) bounds the top_k-th largest class from
 // below.  The few classes at or above the bound are listed -- from the group of vectors that holds a thread's largest, which
 // it has kept in registers, or by reading the thread's vectors again where a second group reaches the bound -- and each takes
-// the place that the number of larger keys in the list says.  Where many classes tie at the top the list does not hold them; then, and for rows with a NaN, each
-// wavefront takes its largest keys one by one and the lists are merged.
+// the place that the number of larger keys in the list says.  Where many classes tie at the top the list does not hold them;
+// then, and for rows with a NaN, each wavefront takes its largest keys one by one and the lists are merged.
 #include <algorithm>
 
 #include "kernels.h"
