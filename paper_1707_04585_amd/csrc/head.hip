@@ -244,9 +244,9 @@ struct Operand {
         if (!ALONG) return v;
         const int lane = (int)threadIdx.x & 63;
         *reinterpret_cast<f4 *>(lds + (lane >> 2) * kPitch + (lane & 3) * 4) = v;
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         v = *reinterpret_cast<const f4 *>(lds + (lane & 15) * kPitch + (lane >> 4) * 4);
-        __builtin_amdgcn_wave_barrier();
+        wave_exchange();
         return v;
     }
 };

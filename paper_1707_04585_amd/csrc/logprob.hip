@@ -269,7 +269,7 @@ struct TeamLds {
 
 template <int NW>
 __device__ __forceinline__ void team_barrier() {
-    if constexpr (NW == 1) __builtin_amdgcn_wave_barrier();
+    if constexpr (NW == 1) wave_exchange();
     else __syncthreads();
 }
 

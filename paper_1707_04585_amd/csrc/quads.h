@@ -59,6 +59,15 @@ __device__ __forceinline__ void store4(float *plane, QuadAt q, f4 v) {
         if (q.owns(j)) plane[q.i + j] = v[j];
 }
 
+// What the wavefront's lanes wrote to LDS before this, any of them reads after it.  A wavefront's LDS accesses are carried out in
+// order, so this costs no instruction and no wait; the fences keep the compiler from moving accesses over the barrier, which by
+// itself orders instructions but not memory.
+__device__ __forceinline__ void wave_exchange() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // Sum over the 64 lanes, in every lane.
 __device__ __forceinline__ double wave_total(double v) {
 #pragma unroll
