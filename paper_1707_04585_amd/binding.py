@@ -10,6 +10,7 @@ point it calls and raises ``RevnetError`` on a negative status.
 from __future__ import annotations
 
 import ctypes as C
+import math
 import os
 import struct
 
@@ -685,9 +686,35 @@ def revnet_body_bwd_stored(desc, tops, dtops, stage_params, down_params, stage_g
     del keep_p, keep_g
 
 
+_HEAD_ARRAYS = ("gamma", "beta", "w", "b")
+
+
 def pack_head(P) -> rvn_head_ptrs:
-    """{gamma, beta, w, b} of device tensors -> rvn_head_params / rvn_head_grads."""
-    return P if isinstance(P, rvn_head_ptrs) else rvn_head_ptrs(*[_ptr(P[k]) for k in ("gamma", "beta", "w", "b")])
+    """{gamma, beta, w, b} of device tensors (float32, contiguous; [c], [c], [classes, c], [classes]) -> rvn_head_params /
+    rvn_head_grads.  Their sizes are compared with the descriptor by the call that takes them."""
+    if isinstance(P, rvn_head_ptrs):
+        return P
+    for name in _HEAD_ARRAYS:
+        dtype = getattr(P[name], "dtype", None)
+        if dtype is not None and _dtype_name(dtype) != "float32":
+            raise ValueError(f"{name} of a head must be float32, not {_dtype_name(dtype)}")
+    out = rvn_head_ptrs(*[_ptr(P[name]) for name in _HEAD_ARRAYS])
+    # (a pointer, or nothing, has no size here)
+    out.sizes = [tuple(P[name].shape) if hasattr(P[name], "shape") else None for name in _HEAD_ARRAYS]
+    return out
+
+
+def _head_ptrs(P, d):
+    """pack_head, its arrays checked against the descriptor d; an rvn_head_ptrs of the caller's own making is taken as it is."""
+    out = pack_head(P)
+    want = [(d.c,), (d.c,), (d.classes, d.c), (d.classes,)]
+    sizes = getattr(out, "sizes", want)
+    if sizes != want:
+        for name, size, shape in zip(_HEAD_ARRAYS, sizes, want):
+            # (a leading or trailing dimension of 1 changes nothing; the weights' rows and columns may not change places)
+            if size is not None and (math.prod(size) != math.prod(shape) or (name == "w" and len(size) == 2 and size != shape)):
+                raise ValueError(f"{name} of a head of {d.c} channels and {d.classes} classes must have the shape {list(shape)}, not {list(size)}")
+    return out
 
 
 def revnet_head_workspace_bytes(desc, n, h, w):
@@ -699,13 +726,15 @@ def revnet_head_workspace_bytes(desc, n, h, w):
 
 
 def revnet_head_fwd(desc, x, params, logits, saved, stream=None):
-    d, p = _desc(desc), pack_head(params)
+    d = _desc(desc)
+    p = _head_ptrs(params, d)
     _check(load_library().revnet_head_fwd(C.byref(d), _tensor_arg(x), C.byref(p), _matrix_arg(logits, "logits")[0], *_ws(saved),
                                           _stream(stream)))
 
 
 def revnet_head_bwd(desc, x, saved, d_logits, params, dx, grads, accumulate_wgrads, ws, stream=None):
-    d, p, g = _desc(desc), pack_head(params), pack_head(grads)
+    d = _desc(desc)
+    p, g = _head_ptrs(params, d), _head_ptrs(grads, d)
     _check(load_library().revnet_head_bwd(C.byref(d), _tensor_arg(x), *_ws(saved), _matrix_arg(d_logits, "d_logits")[0], C.byref(p),
                                           _tensor_arg(dx), C.byref(g), int(accumulate_wgrads), *_ws(ws), _stream(stream)))
 
