@@ -1,5 +1,6 @@
 // Host side of the classification head and of the log probabilities: validation, buffer layouts and the launches.
 #include "api_common.h"
+#include "matrix_overlap.h"
 
 using namespace rvn;
 using namespace rvn::api;
@@ -22,6 +23,11 @@ int check_matrix(const char *name, const rvn_matrix *m, int64_t rows, int64_t co
 
 size_t matrix_bytes(const rvn_matrix *m) {
     return (size_t)((m->rows - 1) * m->ld + m->cols) * (enum_bits(m->dtype) == RVN_F32 ? 4 : 2);
+}
+
+RowBlock rows_of(const rvn_matrix *m) {
+    const int64_t size = enum_bits(m->dtype) == RVN_F32 ? 4 : 2;
+    return RowBlock{(int64_t)reinterpret_cast<uintptr_t>(m->ptr), m->cols * size, m->ld * size, m->rows};
 }
 
 // ---- head --------------------------------------------------------------------------
@@ -192,8 +198,8 @@ int revnet_logprob_bwd(const rvn_matrix *logits, const int64_t *labels, const fl
     if (!labels && !d_entropy) return fail(RVN_ERR_NULL, "neither labels nor d_entropy is given");
     if (d_logprob && !labels) return fail(RVN_ERR_NULL, "d_logprob without labels");
     if (d_entropy && !entropy) return fail(RVN_ERR_NULL, "d_entropy without entropy");
-    if (!(logits->ptr == d_logits->ptr && logits->ld == d_logits->ld) &&
-        ranges_overlap(logits->ptr, matrix_bytes(logits), d_logits->ptr, matrix_bytes(d_logits)))
+    const bool same = logits->ptr == d_logits->ptr && (logits->ld == d_logits->ld || rows == 1);
+    if (!same && row_blocks_overlap(rows_of(logits), rows_of(d_logits)))
         return fail(RVN_ERR_ALIAS, "logits and d_logits overlap");
     Ctx cx;
     cx.stream = static_cast<hipStream_t>(hip_stream);
