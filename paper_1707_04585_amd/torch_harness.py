@@ -252,17 +252,22 @@ class HeadRunner:
         self.logits, self.d_logits = empty(n, classes), empty(n, classes)
         self.logprob, self.entropy, self.lse = empty(n), empty(n), empty(n)
         self.top_ids, self.top_logprob = empty(n, self.top_k, dtype=torch.int64), empty(n, self.top_k)
+        self.scored = False   # whether lse and the other scores are of the logits that are there
 
     def forward(self, x, stream=None):
+        self.scored = False
         B.revnet_head_fwd(self.desc, x, self._pp, self.logits, self.saved, stream)
 
     def score(self, labels, stream=None):
         """labels: int64 [n]; fills logprob, entropy, lse, top_ids and top_logprob."""
         B.revnet_logprob_fwd(self.logits, labels, self.top_k, self.logprob, self.entropy, self.lse, self.top_ids, self.top_logprob,
                              self.ws, stream)
+        self.scored = True
 
     def backward(self, x, labels, dx, accumulate=False, stream=None):
-        """dx, self.grads: derivatives of -mean(logprob), after forward and score."""
+        """dx, self.grads: derivatives of -mean(logprob), after forward; logits that have not been scored since are scored first."""
+        if not self.scored:
+            self.score(labels, stream)
         B.revnet_logprob_bwd(self.logits, labels, self.lse, None, None, None, -1.0 / self.n, self.d_logits, stream)
         B.revnet_head_bwd(self.desc, x, self.saved, self.d_logits, self._pp, dx, self._pg, int(accumulate), self.ws, stream)
 
