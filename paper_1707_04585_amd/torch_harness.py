@@ -282,6 +282,8 @@ class NetRunner:
         self.body = BodyRunner(device=device, **cfg)
         self.head = None
         if head is not None:
+            if self.body.frac_bits:
+                raise ValueError("a head reads floats, and the top of a body in fixed point holds codes")
             top = self.body.tops[-1]
             self.head = HeadRunner(head, *(top.shape[i] for i in (0, 2, 3)), device=device)
         self.device = self.body.device

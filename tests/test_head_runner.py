@@ -43,3 +43,12 @@ def test_the_gradient_is_formed_from_scores_of_the_same_forward_pass(monkeypatch
     r.head.score(lab)
     r.backward(labels=lab)
     assert names(calls) == there + ["logprob_fwd"] + back
+
+
+def test_a_head_on_a_stream_in_fixed_point_is_refused():
+    """The head reads floats; the top of such a body holds codes."""
+    cfg = dict(kind="basic", n=2, h=8, w=8, channels=(16, 32), depths=(1, 1), widths=(None, None), frac_bits=16)
+    stem = dict(w=np.zeros((16, 3, 3, 3)), stride=1, pool=False)
+    with pytest.raises(ValueError):
+        H.NetRunner(cfg, stem, device="cpu", head=head())
+    assert H.NetRunner(cfg, stem, device="cpu").head is None
