@@ -285,7 +285,7 @@ class NetRunner:
             if self.body.frac_bits:
                 raise ValueError("a head reads floats, and the top of a body in fixed point holds codes")
             top = self.body.tops[-1]
-            self.head = HeadRunner(head, *(top.shape[i] for i in (0, 2, 3)), device=device)
+            self.head = HeadRunner(head, *(top.shape[i] for i in (0, 2, 3)), eps=cfg.get("eps", 1e-5), device=device)
         self.device = self.body.device
         c0 = cfg["channels"][0]
         ks = int(stem["w"].shape[2])

@@ -52,3 +52,10 @@ def test_a_head_on_a_stream_in_fixed_point_is_refused():
     with pytest.raises(ValueError):
         H.NetRunner(cfg, stem, device="cpu", head=head())
     assert H.NetRunner(cfg, stem, device="cpu").head is None
+
+
+def test_the_head_of_a_network_has_the_networks_epsilon(monkeypatch):
+    calls = []
+    assert network(monkeypatch, calls).head.desc.bn_eps == 1e-5
+    r = network(monkeypatch, calls, eps=1e-3)
+    assert r.head.desc.bn_eps == 1e-3 and all(st.bn_eps == 1e-3 for st in r.body.desc.stages)
