@@ -622,6 +622,10 @@ int revnet_head_bwd(const rvn_head_desc *desc, const rvn_tensor *x, const void *
  * A logit of -infinity is a class that cannot occur; a row with no other has
  * lse and log probabilities of -infinity and entropy 0.  A row that holds a NaN
  * or +infinity gets NaN for all but its ids (NaN counts as the largest).
+ * Sums are fp32, in an order that follows from the row's alignment, the number
+ * of rows and classes and top_k: the same call gives the same bits, and the same
+ * row in another batch or at another alignment may differ in the last bits of
+ * lse, the log probabilities and entropy (its ids do not).
  * ws: revnet_logprob_workspace_bytes (which may be 0: ws is then not looked
  * at), 256-byte aligned.
  */

@@ -40,12 +40,12 @@ __device__ __forceinline__ double block_total(float v, double *lds) {
 }
 
 // HELD > 0: the channel stays in registers, steps * J <= HELD quads of it in each lane; otherwise it is read three times, the
-// second and third mostly from the caches (whole forward pass at 256 x 512 x 14 x 14 42.2 and 53.7 us).  SINGLE: J == 1, a lane has the
-// same quad of every plane of its (256 x 512 x 7 x 7: 27.1 and 30.8).
+// second and third mostly from the caches (whole forward pass at 256 x 512 x 14 x 14, 100 classes: 42.2 and 53.7 us).  SINGLE: J == 1, a
+// lane has the same quad of every plane of its (256 x 512 x 7 x 7, 1000 classes: 27.1 and 30.8).
 // With d = x - mean and the positive pixels of a plane (as z = x * scale + shift says, as in the backward pass), its sum of
 // ReLU(z) is scale * sum d + beta * count and that of xhat rstd * sum d: one sum and a count a pixel.  (Instructions of this kernel
 // took 21 of its 28 us at 128 x 2048 x 7 x 7 while it formed all three sums pixel by pixel; the whole
-// forward pass took 41.6 us then, 35.0 now.  32 x 2048 x 7 x 7: 12.8 MB in 8.0 us.)
+// forward pass, with 1000 classes, took 41.6 us then, 35.0 now.  32 x 2048 x 7 x 7: 12.8 MB in 8.0 us.)
 template <int TH, int HELD, bool WHOLE, bool SINGLE>
 __global__ __launch_bounds__(TH) void head_pool_k(const float *__restrict__ x, int64_t sn, int64_t sc, const Planes g, float eps,
                                                   const float *__restrict__ gamma, const float *__restrict__ beta,
