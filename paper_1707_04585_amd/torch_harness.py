@@ -300,8 +300,13 @@ class NetRunner:
     def set_params(self, stages, downs):
         self.body.set_params(stages, downs)
 
+    def _check_labels(self, labels):
+        if labels is not None and self.head is None:
+            raise ValueError("labels are scored by a head, and this network has none")
+
     def forward(self, img, stream=None, labels=None):
         """labels (int64 [n], with a head): the head's logits are scored as well."""
+        self._check_labels(labels)
         n, _, h, w = img.shape
         if self.pool and self.conv_out is None:
             ho, wo = (h - 1) // self.stride + 1, (w - 1) // self.stride + 1
@@ -321,6 +326,7 @@ class NetRunner:
     def backward(self, stream=None, labels=None):
         """labels (with a head): derivatives of the mean negative log likelihood;
         otherwise body.dtops[-1] holds the upstream derivative."""
+        self._check_labels(labels)
         if labels is not None:
             self.head.backward(self.body.tops[-1], labels, self.body.dtops[-1], stream=stream)
         self.body.backward(stream=stream)

@@ -59,3 +59,17 @@ def test_the_head_of_a_network_has_the_networks_epsilon(monkeypatch):
     assert network(monkeypatch, calls).head.desc.bn_eps == 1e-5
     r = network(monkeypatch, calls, eps=1e-3)
     assert r.head.desc.bn_eps == 1e-3 and all(st.bn_eps == 1e-3 for st in r.body.desc.stages)
+
+
+def test_labels_for_a_network_without_a_head_are_refused(monkeypatch):
+    calls = []
+    r = network(monkeypatch, calls)
+    r.head = None
+    img, lab = torch.zeros(2, 3, 8, 8), torch.zeros(2, dtype=torch.int64)
+    for call in (lambda: r.forward(img, labels=lab), lambda: r.backward(labels=lab)):
+        with pytest.raises(ValueError):
+            call()
+    assert calls == []
+    r.forward(img)
+    r.backward()
+    assert names(calls) == ["stem_fwd", "body_fwd", "body_bwd", "stem_bwd"]
