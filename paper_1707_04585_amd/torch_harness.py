@@ -252,7 +252,7 @@ class HeadRunner:
         self.logits, self.d_logits = empty(n, classes), empty(n, classes)
         self.logprob, self.entropy, self.lse = empty(n), empty(n), empty(n)
         self.top_ids, self.top_logprob = empty(n, self.top_k, dtype=torch.int64), empty(n, self.top_k)
-        self.scored = False   # whether lse and the other scores are of the logits that are there
+        self.scored = False   # whether lse is of the logits that are there, and no backward pass has used it yet
 
     def forward(self, x, stream=None):
         self.scored = False
@@ -268,6 +268,7 @@ class HeadRunner:
         """dx, self.grads: derivatives of -mean(logprob), after forward; logits that have not been scored since are scored first."""
         if not self.scored:
             self.score(labels, stream)
+        self.scored = False   # (a replayed forward pass, which does not come by here, may follow)
         B.revnet_logprob_bwd(self.logits, labels, self.lse, None, None, None, -1.0 / self.n, self.d_logits, stream)
         B.revnet_head_bwd(self.desc, x, self.saved, self.d_logits, self._pp, dx, self._pg, int(accumulate), self.ws, stream)
 

@@ -43,6 +43,8 @@ def test_the_gradient_is_formed_from_scores_of_the_same_forward_pass(monkeypatch
     r.head.score(lab)
     r.backward(labels=lab)
     assert names(calls) == there + ["logprob_fwd"] + back
+    r.backward(labels=lab)             # what came between may have been a replayed graph: scored again
+    assert names(calls) == ["logprob_fwd"] + back
 
 
 def test_a_head_on_a_stream_in_fixed_point_is_refused():
