@@ -648,9 +648,9 @@ int revnet_logprob_fwd(const rvn_matrix *logits, const int64_t *labels, int32_t 
  * part in the entropy term only; a row whose label is out of range gets NaN.
  * d_logits has the logits' shape and type and may be the same matrix (same ptr
  * and ld) or a block of other columns of the matrix that holds the logits (same
- * ld, no element in common); any other overlap is RVN_ERR_ALIAS, also that of
- * two matrices of different ld, whichever elements they use.  A row of -infinity
- * alone gets zeros, whatever its label.
+ * ld, no element in common); any other overlap is RVN_ERR_ALIAS.  (Two matrices of
+ * different ld overlap where their ranges from first to last element meet.)  A row
+ * of -infinity alone gets zeros, whatever its label.
  */
 int revnet_logprob_bwd(const rvn_matrix *logits, const int64_t *labels, const float *lse, const float *entropy,
                        const float *d_logprob, const float *d_entropy, float scale,
